@@ -391,6 +391,86 @@ hbmm_status hbmm_conv_im2col_static(const void *x, int32_t x_dtype, const hbmm_c
                                     float *C_out, int64_t ldc, void *stream);
 
 /*
+ * 8-bit operands: the layer of Section 5 (fully connected, or any matrix product) with its operands at 8 bits per
+ * element instead of 1 -- for the layers that binarization costs too much accuracy, and for what the backward pass keeps.
+ * The decomposition is the one of Fig. 1 with beta = 128: full-precision scales, one per group, beside a tensor of few
+ * bits, and the product (Eq. 7 regrouped) takes one dot product and one scale product per K-group.
+ *   codes  : e4m3 (no infinities, NaN = 0x7f / 0xff) [rows, ld_codes], ld_codes >= K, a multiple of 16; 16-byte aligned.
+ *            Bytes at columns >= K are neither read as values nor written.
+ *   scales : fp32 [ceil(rows / block_rows), ld_scales], ld_scales >= ceil(K / 128), a multiple of 4; 16-byte aligned.
+ *            Entry (r / block_rows, k / 128) belongs to element (r, k); entries behind the last group are ignored.
+ *   block_rows : 1 (activations, gradients: a scale per group of 128 consecutive row elements) or 128 (weights: a scale
+ *            per block of 128 x 128 elements).
+ * rows and K are below 2^31.  The last group of a row and the last block of a column may be short.
+ */
+typedef struct {
+  int64_t rows;
+  int64_t K;
+  uint8_t *codes;
+  int64_t ld_codes;
+  float *scales;
+  int64_t ld_scales;
+  int32_t block_rows;
+  int32_t reserved;
+} hbmm_fp8_operand;
+
+/* Storage of an 8-bit operand, as hbmm_operand_bytes.  Errors: INVALID_ARG (rows, K <= 0), UNSUPPORTED (block_rows). */
+hbmm_status hbmm_fp8_operand_bytes(int64_t rows, int64_t K, int32_t block_rows, size_t *codes_bytes, size_t *scales_bytes,
+                                   int64_t *ld_codes, int64_t *ld_scales);
+
+/*
+ * Quantization to 8 bits.  Per group or block: amax the largest finite magnitude, scale = the smallest power of two with
+ * amax / scale <= 448 (the largest e4m3 value), at least 2^-117; code = x / scale rounded to nearest even.  x / scale and
+ * code * scale are exact for a power of two, and code * scale is a bf16 number: the backward products below read it
+ * without another rounding.  NaN and infinities become NaN codes and do not count in amax.  -0 becomes +0; a negative
+ * element that rounds to zero keeps its sign bit (hbmm_fp8_binarize_backward takes the element's sign from there).
+ * x: device, [rows, ldx] of x_dtype, ldx >= K, aligned to its element (16-byte aligned rows take vector loads).
+ * out: host descriptor, its buffers filled.  Errors: INVALID_ARG, UNSUPPORTED (block_rows, sizes), ALIGNMENT, CUDA.
+ */
+hbmm_status hbmm_fp8_quantize(const void *x, int32_t x_dtype, int64_t rows, int64_t K, int64_t ldx,
+                              const hbmm_fp8_operand *out, void *stream);
+
+/*
+ * C[m,n] = sum_g sA[m,g] sW[n/128,g] sum_{k in group g} A[m,k] W[n,k]: the forward product of a layer, for one row of A
+ * (a single token) up to long batches.  A: M x K, block_rows 1.  W: N x K, block_rows 128.  Any scales, their product
+ * finite.  A dot product over a group is formed by the tensor cores, groups are summed in fp32.
+ * C: device [M, ldc] of c_dtype (fp32, or bf16 rounded to nearest even), ldc >= N, rows on 16-byte boundaries; fully
+ * overwritten in columns < N.  A NaN code makes its row (of A) or its column (of W) of C NaN and nothing else.
+ * C may not overlap the operands.  Errors: INVALID_ARG, UNSUPPORTED (block_rows, sizes), ALIGNMENT, CUDA.
+ */
+hbmm_status hbmm_fp8_gemm(const hbmm_fp8_operand *A, const hbmm_fp8_operand *W, void *C, int32_t c_dtype, int64_t ldc,
+                          void *stream);
+
+/*
+ * GX[m,k] = sum_g sG[m,g] sW[g,k/128] sum_{n in group g} GY[m,n] W[n,k]: the gradient with respect to the activations.
+ * GY: M x N, block_rows 1 (the gradient of C, quantized along n).  W: N x K, block_rows 128, as the forward product reads it.
+ * GX: device [M, ldgx] of gx_dtype, as C above.  Errors as hbmm_fp8_gemm.
+ */
+hbmm_status hbmm_fp8_input_grad(const hbmm_fp8_operand *GY, const hbmm_fp8_operand *W, void *GX, int32_t gx_dtype,
+                                int64_t ldgx, void *stream);
+
+/*
+ * GW[n,k] = base[n,k] + sum_m gy[m,n] X^[m,k], X^ = codes times scales: the gradient with respect to the weights from the
+ * 8-bit copy of the activations, which is all that the forward pass has to keep of them.
+ * gy: device bf16 [M, ldg], ldg >= N, rows on 16-byte boundaries.  X: M x K, block_rows 1.  X^ enters as bf16: exact for
+ * scales that are powers of two (what hbmm_fp8_quantize writes), otherwise rounded to nearest even.  Sums in fp32.
+ * base: fp32 [N, ld_base] or NULL (zeros); it may be GW itself (same address and leading dimension: the gradient is added
+ * to what is there) and may not overlap it otherwise.  GW: device fp32 [N, ldw], ldw >= K; base and GW rows on 16-byte
+ * boundaries.  Errors: INVALID_ARG, UNSUPPORTED (gy_dtype, block_rows, sizes), ALIGNMENT, CUDA.
+ */
+hbmm_status hbmm_fp8_weight_grad(const void *gy, int32_t gy_dtype, int64_t N, int64_t ldg, const hbmm_fp8_operand *X,
+                                 const float *base, int64_t ld_base, float *GW, int64_t ldw, void *stream);
+
+/*
+ * hbmm_binarize_backward (Eq. 6) from the 8-bit copy of x: X^ = codes times scales stands for x in the group means and in
+ * [|x| <= 1], Sign(x) is the code's sign bit (of every element that hbmm_fp8_quantize wrote the sign of x itself).
+ * X: block_rows 1.  gy, gx: device [rows, ld*] of dtype (both), ld* >= K, aligned to their element.  beta >= 1, any value.
+ * gx may not overlap X or gy.  Errors: INVALID_ARG, UNSUPPORTED (block_rows, sizes), ALIGNMENT, CUDA.
+ */
+hbmm_status hbmm_fp8_binarize_backward(const hbmm_fp8_operand *X, const void *gy, int32_t dtype, int64_t ldg, int32_t beta,
+                                       void *gx, int64_t ldo, void *stream);
+
+/*
  * Device-side health word of the kernels that wait on barriers (the tensor-core contractions and the
  * packed convolution front end).  Their kernels never spin without a limit: a wait that does not
  * complete within the limit records a code, makes the kernel drain what it has in flight, free its
@@ -399,7 +479,8 @@ hbmm_status hbmm_conv_im2col_static(const void *x, int32_t x_dtype, const hbmm_c
  * final drain of the tensor core, 5 epilogue, 6 weight loader, 7 producer waiting for the row factors,
  * 8 the warps that compute them, 9 the self-test of hbmm_debug_expire_wait; reported as they are for
  * the e4m3 HBMM kernel, 100 + code for the HBWN kernel, 200 + code for the packed convolution front end
- * (201 loader, 202-204 compute warps), 300 + code for the folded-scale HBMM kernel.
+ * (201 loader, 202-204 compute warps), 300 + code for the folded-scale HBMM kernel, 400 + code for the
+ * products of 8-bit operands.
  * Lifetime: one word per kernel family and process, holding the FIRST code recorded since it was last
  * cleared; nothing but hbmm_clear_device_error resets it, so after one expiry every later query reports
  * HBMM_ERR_TIMEOUT, whichever call it follows, until the word is cleared.

@@ -6,6 +6,7 @@
 #include <torch/csrc/autograd/python_variable.h>
 #include <torch/csrc/Exceptions.h>
 #include <ATen/ATen.h>
+#include <c10/cuda/CUDAFunctions.h>
 #include <c10/cuda/CUDAStream.h>
 #include "hbmm.h"
 
@@ -18,9 +19,15 @@ decltype(&hbmm_conv_im2col_ex) f_conv;
 decltype(&hbmm_conv_im2col_fused) f_conv_fused;
 decltype(&hbmm_binarize_dense) f_dense;
 decltype(&hbmm_binarize_backward) f_backward;
+decltype(&hbmm_fp8_quantize) f_fp8_quantize;
+decltype(&hbmm_fp8_gemm) f_fp8_gemm;
+decltype(&hbmm_fp8_input_grad) f_fp8_input_grad;
+decltype(&hbmm_fp8_weight_grad) f_fp8_weight_grad;
+decltype(&hbmm_fp8_binarize_backward) f_fp8_backward;
 PyObject* g_error;                 // HbmmError
+PyTypeObject* t_fp8;               // Fp8Operand
 PyTypeObject *t_operand, *t_geom, *t_epilogue;      // the ctypes structures that stand for hbmm_operand, hbmm_conv_geom, hbmm_epilogue
-PyObject *s_desc, *s_cuda_stream;
+PyObject *s_desc, *s_cuda_stream, *s_codes, *s_scales, *s_K, *s_block_rows;
 
 // Arguments of a METH_FASTCALL | METH_KEYWORDS call in the order of `names`; absent ones stay null.
 bool take(const char* what, PyObject* const* args, Py_ssize_t nargs, PyObject* kwnames, const char* const* names, int n, int required, PyObject** out) {
@@ -339,6 +346,206 @@ PyObject* py_binarize_dense(PyObject*, PyObject* const* args, Py_ssize_t nargs, 
   END_HANDLE_TH_ERRORS
 }
 
+// ---- 8-bit operands.  The descriptor is made from the tensors of an Fp8Operand at each call, so that a call takes what they are now.
+
+// Tensors of one call lie on the current device: the launch and the default stream are that device's.
+bool on_current_device(const at::Tensor& t) {
+  if (!t.is_cuda()) {
+    PyErr_SetString(PyExc_ValueError, "device tensor expected");
+    return false;
+  }
+  if (t.get_device() != c10::cuda::current_device()) {
+    PyErr_SetString(PyExc_ValueError, "tensors of the current device expected");
+    return false;
+  }
+  return true;
+}
+// A matrix with contiguous rows; `pitch`: elements between rows, a whole number of 16 bytes for a single row, whose stride says nothing.
+bool matrix(const at::Tensor& t, const char* what, int64_t* pitch) {
+  if (t.dim() != 2 || (t.size(1) > 1 && t.stride(1) != 1)) {
+    PyErr_Format(PyExc_ValueError, "%s must be a matrix with contiguous rows", what);
+    return false;
+  }
+  const int64_t per = 16 / static_cast<int64_t>(t.element_size());
+  *pitch = t.size(0) == 1 ? (t.size(1) + per - 1) / per * per : t.stride(0);
+  return true;
+}
+struct Fp8 {
+  hbmm_fp8_operand d{};
+  PyObject *codes = nullptr, *scales = nullptr;       // held while the call runs
+  ~Fp8() { Py_XDECREF(codes); Py_XDECREF(scales); }
+  bool number(PyObject* o, PyObject* name, long long* v) {
+    PyObject* p = PyObject_GetAttr(o, name);
+    if (!p) return false;
+    const bool ok = integer(p, v);
+    Py_DECREF(p);
+    return ok;
+  }
+  bool open(PyObject* o) {
+    if (!PyObject_TypeCheck(o, t_fp8)) {
+      PyErr_Format(PyExc_TypeError, "Fp8Operand expected, got %s", Py_TYPE(o)->tp_name);
+      return false;
+    }
+    long long K, block_rows;
+    if (!(codes = PyObject_GetAttr(o, s_codes)) || !(scales = PyObject_GetAttr(o, s_scales)) || !number(o, s_K, &K) ||
+        !number(o, s_block_rows, &block_rows))
+      return false;
+    const at::Tensor *c = tensor_of(codes), *s = c ? tensor_of(scales) : nullptr;
+    if (!s) return false;
+    const at::ScalarType ct = c->scalar_type();
+    if ((ct != at::kByte && ct != at::kFloat8_e4m3fn) || s->scalar_type() != at::kFloat) {
+      PyErr_SetString(PyExc_ValueError, "codes must be float8_e4m3fn or uint8, scales float32");
+      return false;
+    }
+    if (!matrix(*c, "codes", &d.ld_codes) || !matrix(*s, "scales", &d.ld_scales)) return false;
+    if (block_rows != 1 && block_rows != 128) {
+      PyErr_SetString(PyExc_ValueError, "block_rows must be 1 or 128");
+      return false;
+    }
+    if (K < 1 || c->size(0) < 1 || c->size(1) < K || s->size(0) < (c->size(0) + block_rows - 1) / block_rows || s->size(1) < (K + 127) / 128) {
+      PyErr_SetString(PyExc_ValueError, "codes or scales are smaller than their operand");
+      return false;
+    }
+    if (!on_current_device(*c) || !on_current_device(*s)) return false;
+    d.rows = c->size(0); d.K = K; d.block_rows = static_cast<int32_t>(block_rows);
+    d.codes = static_cast<uint8_t*>(c->data_ptr());
+    d.scales = static_cast<float*>(s->data_ptr());
+    return true;
+  }
+};
+// A tensor argument of the given extents.
+const at::Tensor* sized(PyObject* o, const char* what, int64_t rows, int64_t cols, int64_t* pitch) {
+  const at::Tensor* t = tensor_of(o);
+  if (!t || !matrix(*t, what, pitch)) return nullptr;
+  if (t->size(0) != rows || t->size(1) != cols) {
+    PyErr_Format(PyExc_ValueError, "%s must be [%lld, %lld]", what, static_cast<long long>(rows), static_cast<long long>(cols));
+    return nullptr;
+  }
+  return on_current_device(*t) ? t : nullptr;
+}
+
+PyObject* py_fp8_quantize(PyObject*, PyObject* const* args, Py_ssize_t nargs, PyObject* kw) {
+  HANDLE_TH_ERRORS
+  static const char* const names[] = {"x", "out", "stream"};
+  PyObject* a[3];
+  Fp8 out;
+  if (!take("fp8_quantize", args, nargs, kw, names, 3, 2, a) || !out.open(a[1])) return nullptr;
+  int64_t ld;
+  int32_t dt;
+  void* s;
+  const at::Tensor* x = sized(a[0], "x", out.d.rows, out.d.K, &ld);
+  if (!x || !dtype_code(*x, &dt) || !stream_of(a[2], &s)) return nullptr;
+  const void* p = x->data_ptr();
+  HBMM_CALL(f_fp8_quantize(p, dt, out.d.rows, out.d.K, ld, &out.d, s));
+  return done(status, "hbmm_fp8_quantize", a[1]);
+  END_HANDLE_TH_ERRORS
+}
+
+PyObject* fp8_product(const char* where, bool transposed, PyObject** a) {
+  Fp8 A, W;
+  if (!A.open(a[0]) || !W.open(a[1])) return nullptr;
+  int64_t ld;
+  int32_t dt;
+  void* s;
+  const at::Tensor* C = sized(a[2], transposed ? "GX" : "C", A.d.rows, transposed ? W.d.K : W.d.rows, &ld);
+  if (!C || !dtype_code(*C, &dt) || !stream_of(a[3], &s)) return nullptr;
+  void* p = C->data_ptr();
+  HBMM_CALL((transposed ? f_fp8_input_grad : f_fp8_gemm)(&A.d, &W.d, p, dt, ld, s));
+  return done(status, where, a[2]);
+}
+PyObject* py_fp8_gemm(PyObject*, PyObject* const* args, Py_ssize_t nargs, PyObject* kw) {
+  HANDLE_TH_ERRORS
+  static const char* const names[] = {"A", "W", "C", "stream"};
+  PyObject* a[4];
+  return take("fp8_gemm", args, nargs, kw, names, 4, 3, a) ? fp8_product("hbmm_fp8_gemm", false, a) : nullptr;
+  END_HANDLE_TH_ERRORS
+}
+PyObject* py_fp8_input_grad(PyObject*, PyObject* const* args, Py_ssize_t nargs, PyObject* kw) {
+  HANDLE_TH_ERRORS
+  static const char* const names[] = {"GY", "W", "GX", "stream"};
+  PyObject* a[4];
+  return take("fp8_input_grad", args, nargs, kw, names, 4, 3, a) ? fp8_product("hbmm_fp8_input_grad", true, a) : nullptr;
+  END_HANDLE_TH_ERRORS
+}
+
+PyObject* py_fp8_weight_grad(PyObject*, PyObject* const* args, Py_ssize_t nargs, PyObject* kw) {
+  HANDLE_TH_ERRORS
+  static const char* const names[] = {"gy", "X", "GW", "base", "stream"};
+  PyObject* a[5];
+  Fp8 X;
+  if (!take("fp8_weight_grad", args, nargs, kw, names, 5, 3, a) || !X.open(a[1])) return nullptr;
+  const at::Tensor *gy = tensor_of(a[0]), *gw = gy ? tensor_of(a[2]) : nullptr, *base = nullptr;
+  if (!gw || gw->dim() != 2) {
+    if (gw) PyErr_SetString(PyExc_ValueError, "GW must be a matrix with contiguous rows");
+    return nullptr;
+  }
+  const int64_t N = gw->size(0);
+  int64_t ldg, ldw, ldb = 0;
+  int32_t dt;
+  void* s;
+  if (!sized(a[0], "gy", X.d.rows, N, &ldg) || !sized(a[2], "GW", N, X.d.K, &ldw) || !dtype_code(*gy, &dt)) return nullptr;
+  if (!none(a[3]) && !(base = sized(a[3], "base", N, X.d.K, &ldb))) return nullptr;
+  if (gw->scalar_type() != at::kFloat || (base && base->scalar_type() != at::kFloat)) {
+    PyErr_SetString(PyExc_ValueError, "GW and base must be float32");
+    return nullptr;
+  }
+  if (!stream_of(a[4], &s)) return nullptr;
+  const void* pg = gy->data_ptr();
+  const float* pb = base ? static_cast<const float*>(base->data_ptr()) : nullptr;
+  float* pw = static_cast<float*>(gw->data_ptr());
+  HBMM_CALL(f_fp8_weight_grad(pg, dt, N, ldg, &X.d, pb, ldb, pw, ldw, s));
+  return done(status, "hbmm_fp8_weight_grad", a[2]);
+  END_HANDLE_TH_ERRORS
+}
+
+PyObject* py_fp8_binarize_backward(PyObject*, PyObject* const* args, Py_ssize_t nargs, PyObject* kw) {
+  HANDLE_TH_ERRORS
+  static const char* const names[] = {"X", "gy", "beta", "gx", "stream"};
+  PyObject* a[5];
+  Fp8 X;
+  if (!take("fp8_binarize_backward", args, nargs, kw, names, 5, 3, a) || !X.open(a[0])) return nullptr;
+  int64_t ldg, ldo;
+  int32_t dt, beta;
+  void* s;
+  const at::Tensor* gy = sized(a[1], "gy", X.d.rows, X.d.K, &ldg);
+  if (!gy || !dtype_code(*gy, &dt)) return nullptr;
+  PyObject* result = a[3];
+  if (none(result)) {
+    const at::Tensor own = at::empty(gy->sizes(), gy->options());
+    if (!(result = THPVariable_Wrap(own))) return nullptr;
+  } else {
+    Py_INCREF(result);
+  }
+  const Owned keep{result};
+  const at::Tensor* gx = sized(result, "gx", X.d.rows, X.d.K, &ldo);
+  if (!gx) return nullptr;
+  if (gx->scalar_type() != gy->scalar_type()) {
+    PyErr_SetString(PyExc_ValueError, "gx must have gy's type");
+    return nullptr;
+  }
+  if (!small_integer(a[2], &beta) || !stream_of(a[4], &s)) return nullptr;
+  const void* pg = gy->data_ptr();
+  void* po = gx->data_ptr();
+  HBMM_CALL(f_fp8_backward(&X.d, pg, dt, ldg, beta, po, ldo, s));
+  return done(status, "hbmm_fp8_binarize_backward", result);
+  END_HANDLE_TH_ERRORS
+}
+
+// connect_fp8(Fp8Operand, addresses of the C functions in the order of the f_fp8 pointers above)
+PyObject* py_connect_fp8(PyObject*, PyObject* args) {
+  PyObject* type;
+  unsigned long long p[5];
+  if (!PyArg_ParseTuple(args, "O!KKKKK", &PyType_Type, &type, &p[0], &p[1], &p[2], &p[3], &p[4])) return nullptr;
+  f_fp8_quantize = reinterpret_cast<decltype(f_fp8_quantize)>(p[0]);
+  f_fp8_gemm = reinterpret_cast<decltype(f_fp8_gemm)>(p[1]);
+  f_fp8_input_grad = reinterpret_cast<decltype(f_fp8_input_grad)>(p[2]);
+  f_fp8_weight_grad = reinterpret_cast<decltype(f_fp8_weight_grad)>(p[3]);
+  f_fp8_backward = reinterpret_cast<decltype(f_fp8_backward)>(p[4]);
+  Py_INCREF(type);
+  Py_XSETREF(t_fp8, reinterpret_cast<PyTypeObject*>(type));
+  Py_RETURN_NONE;
+}
+
 // connect(HbmmError, hbmm_operand, hbmm_conv_geom, hbmm_epilogue, addresses of the C functions in the order of the f_ pointers above)
 PyObject* py_connect(PyObject*, PyObject* args) {
   PyObject *err, *types[3];
@@ -383,7 +590,22 @@ PyMethodDef methods[] = {
     {"binarize_backward", FAST(py_binarize_backward),
      "binarize_backward($module, /, x, gy, beta, gx=None, stream=None)\n--\n\n"
      "hbmm_binarize_backward: x, gy fp32 [rows, K] (row stride >= K, unit column stride); returns gx = dC/dX."},
+    {"fp8_quantize", FAST(py_fp8_quantize),
+     "fp8_quantize($module, /, x, out, stream=None)\n--\n\n"
+     "hbmm_fp8_quantize: x [rows, K] fp32 / bf16 into the Fp8Operand ``out``, which is returned."},
+    {"fp8_gemm", FAST(py_fp8_gemm),
+     "fp8_gemm($module, /, A, W, C, stream=None)\n--\n\nhbmm_fp8_gemm: C[M, N] (fp32 / bf16, caller-allocated) = A^ W^^T."},
+    {"fp8_input_grad", FAST(py_fp8_input_grad),
+     "fp8_input_grad($module, /, GY, W, GX, stream=None)\n--\n\nhbmm_fp8_input_grad: GX[M, K] (fp32 / bf16, caller-allocated) = GY^ W^."},
+    {"fp8_weight_grad", FAST(py_fp8_weight_grad),
+     "fp8_weight_grad($module, /, gy, X, GW, base=None, stream=None)\n--\n\n"
+     "hbmm_fp8_weight_grad: GW[N, K] (fp32, caller-allocated) = gy^T X^ (+ base, which may be GW); gy bf16 [M, N], X the 8-bit copy of the\n"
+     "activations."},
+    {"fp8_binarize_backward", FAST(py_fp8_binarize_backward),
+     "fp8_binarize_backward($module, /, X, gy, beta, gx=None, stream=None)\n--\n\n"
+     "hbmm_fp8_binarize_backward: binarize_backward from the 8-bit copy X of x; gy, gx [rows, K] fp32 / bf16."},
     {"connect", py_connect, METH_VARARGS, nullptr},
+    {"connect_fp8", py_connect_fp8, METH_VARARGS, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module_def = {PyModuleDef_HEAD_INIT, "_binding", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
@@ -392,7 +614,11 @@ PyModuleDef module_def = {PyModuleDef_HEAD_INIT, "_binding", nullptr, -1, method
 PyMODINIT_FUNC PyInit__binding() {
   s_desc = PyUnicode_InternFromString("desc");
   s_cuda_stream = PyUnicode_InternFromString("cuda_stream");
-  if (!s_desc || !s_cuda_stream) return nullptr;
+  s_codes = PyUnicode_InternFromString("codes");
+  s_scales = PyUnicode_InternFromString("scales");
+  s_K = PyUnicode_InternFromString("K");
+  s_block_rows = PyUnicode_InternFromString("block_rows");
+  if (!s_desc || !s_cuda_stream || !s_codes || !s_scales || !s_K || !s_block_rows) return nullptr;
   PyObject* m = PyModule_Create(&module_def);
   if (m && PyModule_AddStringConstant(m, "BUILT_FOR", HBMM_BUILT_FOR) != 0) Py_CLEAR(m);
   return m;

@@ -1,0 +1,210 @@
+// Gradient through the Hadamard binarization (Eq. 6, straight-through estimator of Eq. 5) from an 8-bit copy of x:
+//   gx[i] = (1/n_g) s_i sum_{j in group(i)} gy[j] s_j  +  delta_g gy[i] [|x^_i| <= 1],
+// x^ = code * scale (exact in fp32 for the quantizer's scales), s the code's sign bit, delta_g the mean |x^| of the group.
+// A stream: 1 + 4 + 4 bytes per element (1 + 2 + 2 in bf16) where the fp32 form of backward.cu moves 12.
+//
+// Groups of a power of two up to 128 elements: the 128 elements that share a scale belong to 32 lanes of four (fp32) or 16 lanes
+// of eight (bf16): 16-byte gradients either way; group sums are shuffle trees inside them.
+// Other groups: a team of 2^t lanes per group, or a CTA per group of more than 1024, two walks over the group.
+#include <cuda_bf16.h>
+#include "fp8_common.cuh"
+#include "kernels.h"
+#include "pdl.cuh"
+#include "row_io.cuh"
+
+namespace hbmm {
+namespace {
+
+using namespace fp8;
+
+constexpr int kThreads = 256;
+
+struct BackArgs {
+  const uint8_t* codes; const float* scales;
+  int64_t rows, K, ld, ld_s;
+  const void* gy; int64_t ldg;
+  void* gx; int64_t ldo;
+};
+
+__device__ __forceinline__ float with_sign(float v, uint32_t code) { return __uint_as_float(__float_as_uint(v) ^ ((code & 0x80u) << 24)); }
+template <typename T> __device__ __forceinline__ T rounded(float v);
+template <> __device__ __forceinline__ float rounded<float>(float v) { return v; }
+template <> __device__ __forceinline__ __nv_bfloat16 rounded<__nv_bfloat16>(float v) { return __float2bfloat16_rn(v); }
+
+// Elements per lane.
+template <typename T> struct Per { static constexpr int N = 16 / sizeof(T); };
+
+template <typename T, int BETA, bool VEC>
+__global__ void __launch_bounds__(kThreads)
+fp8_binarize_backward_rows(const BackArgs a) {
+  constexpr int E = Per<T>::N, RUN = 32 * E;                         // a warp's run: one scale group (fp32) or two (bf16)
+  constexpr int IN = BETA < E ? BETA : E, LANES = BETA > E ? BETA / E : 1;
+  pdl_wait();
+  const int lane = threadIdx.x & 31;
+  const int64_t chunks = (a.K + RUN - 1) / RUN, items = a.rows * chunks;
+  const int64_t nwarps = static_cast<int64_t>(gridDim.x) * (kThreads / 32);
+  for (int64_t it = (static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x) >> 5; it < items; it += nwarps) {    // warp-uniform
+    const int64_t r = it / chunks, k = (it - r * chunks) * RUN + lane * E;
+    const T* gy = static_cast<const T*>(a.gy) + r * a.ldg;
+    T* gx = static_cast<T*>(a.gx) + r * a.ldo;
+    const uint8_t* codes = a.codes + r * a.ld;
+    const bool whole = k + E <= a.K;
+    uint32_t c[E / 4] = {};
+    float g[E];
+    const float scale = k < a.K ? loadf(a.scales + r * a.ld_s + k / kGroup) : 0.0f;
+    if (whole) {                                                     // codes start on 16 bytes and k is a multiple of E
+      if constexpr (E == 8) { const uint2 q = load8(codes + k); c[0] = q.x; c[1] = q.y; }
+      else c[0] = load4(codes + k);
+    } else {
+#pragma unroll
+      for (int e = 0; e < E; e++)
+        if (k + e < a.K) c[e / 4] |= load1(codes + k + e) << (8 * (e % 4));
+    }
+    if (VEC && whole) {
+      const uint4 q = load16(gy + k);
+      const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+      for (int i = 0; i < 4; i++) {
+        if constexpr (E == 8) { g[2 * i] = __uint_as_float(w[i] << 16); g[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u); }
+        else g[i] = __uint_as_float(w[i]);
+      }
+    } else {
+#pragma unroll
+      for (int e = 0; e < E; e++) g[e] = k + e < a.K ? load_elem<T>(gy + k + e) : 0.0f;
+    }
+    float mag[E], back[E];                                           // |x^| and gy s
+#pragma unroll
+    for (int e = 0; e < E; e += 2) {
+      const float2 f = from_e4m3x2((c[e / 4] & 0x7F7F7F7Fu) >> (8 * (e % 4)));
+      mag[e] = f.x * scale; mag[e + 1] = f.y * scale;
+    }
+#pragma unroll
+    for (int e = 0; e < E; e++) back[e] = with_sign(g[e], c[e / 4] >> (8 * (e % 4)));
+    float o[E];
+#pragma unroll
+    for (int q = 0; q < E; q += IN) {                                // the groups of this lane
+      float m[IN], b[IN];
+#pragma unroll
+      for (int e = 0; e < IN; e++) { m[e] = mag[q + e]; b[e] = back[q + e]; }
+#pragma unroll
+      for (int w = 1; w < IN; w <<= 1)
+#pragma unroll
+        for (int e = 0; e < IN; e += 2 * w) { m[e] += m[e + w]; b[e] += b[e + w]; }
+      float sm = m[0], sb = b[0];
+#pragma unroll
+      for (int off = 1; off < LANES; off <<= 1) {
+        sm += __shfl_xor_sync(0xffffffffu, sm, off);
+        sb += __shfl_xor_sync(0xffffffffu, sb, off);
+      }
+      const int64_t left = a.K - (k + q) / BETA * BETA;              // elements from the group's start on
+      float dm, db;
+      if (left >= BETA) { dm = sm * (1.0f / BETA); db = sb * (1.0f / BETA); }
+      else { const float n = static_cast<float>(left > 0 ? left : 1); dm = sm / n; db = sb / n; }
+#pragma unroll
+      for (int e = q; e < q + IN; e++) o[e] = with_sign(db, c[e / 4] >> (8 * (e % 4))) + (mag[e] <= 1.0f ? dm * g[e] : 0.0f);
+    }
+    if (VEC && whole) {
+      if constexpr (E == 8) {
+        *reinterpret_cast<uint4*>(gx + k) = make_uint4(rowio::bf16_pair(o[0], o[1]), rowio::bf16_pair(o[2], o[3]),
+                                                       rowio::bf16_pair(o[4], o[5]), rowio::bf16_pair(o[6], o[7]));
+      } else {
+        *reinterpret_cast<float4*>(gx + k) = make_float4(o[0], o[1], o[2], o[3]);
+      }
+    } else {
+#pragma unroll
+      for (int e = 0; e < E; e++)
+        if (k + e < a.K) gx[k + e] = rounded<T>(o[e]);
+    }
+  }
+}
+
+__device__ __forceinline__ float magnitude(uint32_t code, float scale) { return from_e4m3x2(code & 0x7Fu).x * scale; }
+
+// A team of TEAM threads (at most a warp, or the whole CTA) per (row, group), any group length.
+template <typename T, int TEAM>
+__global__ void __launch_bounds__(kThreads)
+fp8_binarize_backward_teams(const BackArgs a, int64_t beta) {
+  constexpr int WARPS = kThreads / 32;
+  __shared__ float part[2][WARPS];
+  pdl_wait();
+  const int64_t G = (a.K + beta - 1) / beta, items = a.rows * G;
+  const int me = threadIdx.x % TEAM;
+  constexpr int TEAMS = kThreads / TEAM;
+  const int64_t step = static_cast<int64_t>(gridDim.x) * TEAMS;
+  // whole CTAs walk together (the shuffles need every lane, the barriers every warp): the bound is rounded up
+  for (int64_t first = static_cast<int64_t>(blockIdx.x) * TEAMS; first < items; first += step) {
+    const int64_t it = first + threadIdx.x / TEAM;
+    const bool live = it < items;
+    const int64_t r = live ? it / G : 0, k0 = live ? (it - r * G) * beta : 0;
+    const int64_t k1 = live ? (k0 + beta < a.K ? k0 + beta : a.K) : 0;
+    const T* gy = static_cast<const T*>(a.gy) + r * a.ldg;
+    T* gx = static_cast<T*>(a.gx) + r * a.ldo;
+    const uint8_t* codes = a.codes + r * a.ld;
+    const float* scales = a.scales + r * a.ld_s;
+    float sm = 0.0f, sb = 0.0f;
+    for (int64_t k = k0 + me; k < k1; k += TEAM) {
+      const uint32_t c = load1(codes + k);
+      sm += magnitude(c, loadf(scales + k / kGroup));
+      sb += with_sign(load_elem<T>(gy + k), c);
+    }
+#pragma unroll
+    for (int off = 1; off < (TEAM < 32 ? TEAM : 32); off <<= 1) {
+      sm += __shfl_xor_sync(0xffffffffu, sm, off);
+      sb += __shfl_xor_sync(0xffffffffu, sb, off);
+    }
+    if constexpr (TEAM > 32) {
+      __syncthreads();                                               // the group before has been read
+      if (threadIdx.x % 32 == 0) { part[0][threadIdx.x / 32] = sm; part[1][threadIdx.x / 32] = sb; }
+      __syncthreads();
+      sm = sb = 0.0f;
+#pragma unroll
+      for (int w = 0; w < WARPS; w++) { sm += part[0][w]; sb += part[1][w]; }
+    }
+    const float n = static_cast<float>(k1 > k0 ? k1 - k0 : 1), dm = sm / n, db = sb / n;
+    for (int64_t k = k0 + me; k < k1; k += TEAM) {
+      const uint32_t c = load1(codes + k);
+      const float ste = magnitude(c, loadf(scales + k / kGroup)) <= 1.0f ? dm * load_elem<T>(gy + k) : 0.0f;
+      gx[k] = rounded<T>(with_sign(db, c) + ste);
+    }
+  }
+}
+
+template <typename T>
+cudaError_t launch(const BackArgs& a, int64_t beta, int sms, cudaStream_t stream) {
+  const int64_t cap = static_cast<int64_t>(sms) * 32;
+  const auto grid = [&](int64_t work, int64_t per) {
+    const int64_t n = (work + per - 1) / per;
+    return dim3(static_cast<unsigned>(n < cap ? n : cap));
+  };
+  // group sizes a warp takes by shuffles (a row shorter than its group has a last group of its own length like any other)
+  if ((beta & (beta - 1)) == 0 && beta <= 128) {
+    const int64_t run = 32 * Per<T>::N;
+    const dim3 g = grid(a.rows * ((a.K + run - 1) / run), kThreads / 32);
+    const bool vec = reinterpret_cast<uintptr_t>(a.gy) % 16 == 0 && reinterpret_cast<uintptr_t>(a.gx) % 16 == 0 &&
+                     a.ldg * static_cast<int64_t>(sizeof(T)) % 16 == 0 && a.ldo * static_cast<int64_t>(sizeof(T)) % 16 == 0;
+#define HBMM_B(B)                                                                                                                   \
+  case B:                                                                                                                           \
+    return vec ? launch_pdl(fp8_binarize_backward_rows<T, B, true>, g, dim3(kThreads), 0, stream, a)                                 \
+               : launch_pdl(fp8_binarize_backward_rows<T, B, false>, g, dim3(kThreads), 0, stream, a);
+    switch (beta) { HBMM_B(1) HBMM_B(2) HBMM_B(4) HBMM_B(8) HBMM_B(16) HBMM_B(32) HBMM_B(64) HBMM_B(128) }
+#undef HBMM_B
+  }
+  if (beta > a.K) beta = a.K;
+  const int64_t items = a.rows * ((a.K + beta - 1) / beta);
+  if (beta > 1024) return launch_pdl(fp8_binarize_backward_teams<T, kThreads>, grid(items, 1), dim3(kThreads), 0, stream, a, beta);
+  if (beta > 16) return launch_pdl(fp8_binarize_backward_teams<T, 32>, grid(items, kThreads / 32), dim3(kThreads), 0, stream, a, beta);
+  return launch_pdl(fp8_binarize_backward_teams<T, 4>, grid(items, kThreads / 4), dim3(kThreads), 0, stream, a, beta);
+}
+
+}  // namespace
+
+cudaError_t launch_fp8_binarize_backward(const Fp8View& X, const void* gy, bool bf16, int64_t ldg, int64_t beta, void* gx, int64_t ldo,
+                                         cudaStream_t stream) {
+  int dev = 0, sms = 0;
+  const cudaError_t e = current_device(&dev, &sms);
+  if (e != cudaSuccess) return e;
+  const BackArgs a{X.codes, X.scales, X.rows, X.K, X.ld, X.ld_s, gy, ldg, gx, ldo};
+  return bf16 ? launch<__nv_bfloat16>(a, beta, sms, stream) : launch<float>(a, beta, sms, stream);
+}
+
+}  // namespace hbmm

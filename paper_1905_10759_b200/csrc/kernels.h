@@ -237,6 +237,21 @@ cudaError_t im2col_tma_health(int op, int* value);
 // sink: device, at least blocks * 1024 words (never written in practice).
 cudaError_t launch_alu_rate(int kind, int blocks, int iters, uint32_t* sink, int64_t* ops, cudaStream_t stream);
 
+// 8-bit operands (fp8_*.cu): e4m3 codes with one fp32 scale per 128 row elements (block_rows 1) or 128 x 128 block (128).
+struct Fp8View {
+  const uint8_t* codes;   // [rows, ld]
+  const float* scales;    // [ceil(rows / block_rows), ld_s]
+  int64_t rows, K, ld, ld_s;
+};
+cudaError_t launch_fp8_quantize(const void* x, bool x_bf16, int64_t rows, int64_t K, int64_t ldx, uint8_t* codes, int64_t ld, float* scales,
+                                int64_t ld_s, bool blocks, cudaStream_t stream);
+// C = A^ W^^T (transposed: C = A^ W^, the contraction along the rows of W).
+cudaError_t launch_fp8_gemm(const Fp8View& A, const Fp8View& W, bool transposed, void* C, bool c_bf16, int64_t ldc, cudaStream_t stream);
+cudaError_t launch_fp8_weight_grad(const void* gy, int64_t N, int64_t ldg, const Fp8View& X, const float* base, int64_t ld_base, float* gw,
+                                   int64_t ldw, cudaStream_t stream);
+cudaError_t launch_fp8_binarize_backward(const Fp8View& X, const void* gy, bool bf16, int64_t ldg, int64_t beta, void* gx, int64_t ldo,
+                                         cudaStream_t stream);
+
 cudaError_t launch_im2col_bf16(const void* x, int x_bf16, const ConvGeom& g, void* out, int64_t ld,
                                cudaStream_t stream);
 

@@ -46,6 +46,8 @@ EXPORTS = [
     "hbmm_binarize_backward", "hbmm_gemm_binarize_next", "hbmm_binarize_dense",
     "hbmm_clear_device_error", "hbmm_debug_set_wait_limit", "hbmm_debug_expire_wait", "hbmm_bench_alu_rate",
     "hbmm_gemm_fused", "hbmm_conv_im2col_fused",
+    "hbmm_fp8_operand_bytes", "hbmm_fp8_quantize", "hbmm_fp8_gemm", "hbmm_fp8_input_grad", "hbmm_fp8_weight_grad",
+    "hbmm_fp8_binarize_backward",
 ]
 STATIC_SCRATCH_BYTES = 32 << 20
 
@@ -371,3 +373,60 @@ def gemm_fused(A: Operand, W: Operand, ep: hbmm_epilogue, workspace: torch.Tenso
     """hbmm_gemm_fused: the product goes through activation, affine map and dense / binarized output in the epilogue."""
     _check(_lib.hbmm_gemm_fused(ctypes.byref(A.desc), ctypes.byref(W.desc), ctypes.byref(ep), _dev_ptr(workspace),
                                 workspace.numel() * workspace.element_size(), _stream(stream)), "hbmm_gemm_fused")
+
+
+class hbmm_fp8_operand(ctypes.Structure):
+    _fields_ = [
+        ("rows", ctypes.c_int64), ("K", ctypes.c_int64),
+        ("codes", ctypes.c_void_p), ("ld_codes", ctypes.c_int64),
+        ("scales", ctypes.c_void_p), ("ld_scales", ctypes.c_int64),
+        ("block_rows", ctypes.c_int32), ("reserved", ctypes.c_int32),
+    ]
+
+
+_lib.hbmm_fp8_operand_bytes.argtypes = [_i64, _i64, _i32, _P(_sz), _P(_sz), _P(_i64), _P(_i64)]
+_lib.hbmm_fp8_quantize.argtypes = [_vp, _i32, _i64, _i64, _i64, _P(hbmm_fp8_operand), _vp]
+_lib.hbmm_fp8_gemm.argtypes = _lib.hbmm_fp8_input_grad.argtypes = [_P(hbmm_fp8_operand), _P(hbmm_fp8_operand), _vp, _i32, _i64, _vp]
+_lib.hbmm_fp8_weight_grad.argtypes = [_vp, _i32, _i64, _i64, _P(hbmm_fp8_operand), _vp, _i64, _vp, _i64, _vp]
+_lib.hbmm_fp8_binarize_backward.argtypes = [_P(hbmm_fp8_operand), _vp, _i32, _i64, _i32, _vp, _i64, _vp]
+for _n in EXPORTS:
+    if _n.startswith("hbmm_fp8_"):
+        getattr(_lib, _n).restype = _i32
+
+
+@dataclass(slots=True)
+class Fp8Operand:
+    """A matrix [rows, K] in 8 bits: ``codes`` [rows, >= K] float8_e4m3fn (or uint8) and ``scales`` float32, one per 128 consecutive
+    elements of a row (block_rows 1: activations, gradients) or per block of 128 x 128 elements (block_rows 128: weights).
+    Rows of both start on 16-byte boundaries.  Calls read the tensors' addresses and sizes when they are made."""
+    codes: torch.Tensor
+    scales: torch.Tensor
+    K: int
+    block_rows: int = 1
+
+    @property
+    def rows(self) -> int:
+        return self.codes.shape[0]
+
+
+def fp8_operand_bytes(rows: int, K: int, block_rows: int = 1):
+    """hbmm_fp8_operand_bytes -> (codes_bytes, scales_bytes, ld_codes, ld_scales)."""
+    cb, sb, lc, ls = _sz(), _sz(), _i64(), _i64()
+    _check(_lib.hbmm_fp8_operand_bytes(rows, K, block_rows, cb, sb, lc, ls), "hbmm_fp8_operand_bytes")
+    return cb.value, sb.value, lc.value, ls.value
+
+
+def alloc_fp8_operand(rows: int, K: int, block_rows: int = 1, device="cuda") -> Fp8Operand:
+    """Allocate the buffers of an 8-bit operand (sizes from hbmm_fp8_operand_bytes)."""
+    _, _, lc, ls = fp8_operand_bytes(rows, K, block_rows)
+    return Fp8Operand(torch.empty((rows, lc), dtype=torch.float8_e4m3fn, device=device),
+                      torch.empty((-(-rows // block_rows), ls), dtype=torch.float32, device=device), K, block_rows)
+
+
+_binding.connect_fp8(Fp8Operand, *(ctypes.cast(getattr(_lib, _n), ctypes.c_void_p).value for _n in (
+    "hbmm_fp8_quantize", "hbmm_fp8_gemm", "hbmm_fp8_input_grad", "hbmm_fp8_weight_grad", "hbmm_fp8_binarize_backward")))
+fp8_quantize = _binding.fp8_quantize
+fp8_gemm = _binding.fp8_gemm
+fp8_input_grad = _binding.fp8_input_grad
+fp8_weight_grad = _binding.fp8_weight_grad
+fp8_binarize_backward = _binding.fp8_binarize_backward
