@@ -540,6 +540,9 @@ hbmm_status hbmm_last_device_error(int32_t* code) {
   int c4 = 0;
   if (gemm_fold_health(kHealthRead, &c4) != cudaSuccess) return HBMM_ERR_CUDA;
   if (c == 0 && c4 != 0) c = 300 + c4;    // the folded-scale HBMM kernel: 301..309
+  int c5 = 0;
+  if (fp8_gemm_health(kHealthRead, &c5) != cudaSuccess) return HBMM_ERR_CUDA;
+  if (c == 0 && c5 != 0) c = 400 + c5;    // the products of 8-bit operands
   if (code) *code = c;
   return c == 0 ? HBMM_OK : HBMM_ERR_TIMEOUT;
 }
@@ -547,7 +550,8 @@ hbmm_status hbmm_last_device_error(int32_t* code) {
 hbmm_status hbmm_clear_device_error(void) {
   int unused = 0;
   if (gemm_umma_health(kHealthClear, &unused) != cudaSuccess || hbwn_umma_health(kHealthClear, &unused) != cudaSuccess ||
-      im2col_tma_health(kHealthClear, &unused) != cudaSuccess || gemm_fold_health(kHealthClear, &unused) != cudaSuccess)
+      im2col_tma_health(kHealthClear, &unused) != cudaSuccess || gemm_fold_health(kHealthClear, &unused) != cudaSuccess ||
+      fp8_gemm_health(kHealthClear, &unused) != cudaSuccess)
     return HBMM_ERR_CUDA;
   return HBMM_OK;
 }
@@ -556,7 +560,8 @@ hbmm_status hbmm_debug_set_wait_limit(uint32_t polls) {
   int v = static_cast<int>(polls);
   if (polls > 0x7FFFFFFFu) return HBMM_ERR_INVALID_ARG;
   if (gemm_umma_health(kHealthSetSpinLimit, &v) != cudaSuccess || hbwn_umma_health(kHealthSetSpinLimit, &v) != cudaSuccess ||
-      im2col_tma_health(kHealthSetSpinLimit, &v) != cudaSuccess || gemm_fold_health(kHealthSetSpinLimit, &v) != cudaSuccess)
+      im2col_tma_health(kHealthSetSpinLimit, &v) != cudaSuccess || gemm_fold_health(kHealthSetSpinLimit, &v) != cudaSuccess ||
+      fp8_gemm_health(kHealthSetSpinLimit, &v) != cudaSuccess)
     return HBMM_ERR_CUDA;
   return HBMM_OK;
 }

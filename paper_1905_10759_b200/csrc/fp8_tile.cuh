@@ -1,0 +1,158 @@
+// Epilogue of the 8-bit operands' tensor-core products: partial sums of a run of the contraction leave tensor memory into fp32
+// registers (one row per thread), finished tiles leave through shared memory in whole lines, and the parts of a tile that several
+// CTA pairs of a cluster share are added over distributed shared memory in rank order (no atomics: the same sum in every run).
+#pragma once
+#include <cuda_bf16.h>
+#include "fp8_common.cuh"
+#include "umma_common.cuh"
+
+namespace hbmm {
+namespace fp8 {
+
+using namespace umma;
+
+// Where a product goes: [M, N] fp32 or bf16, rows on 16-byte boundaries; base (fp32, may be null) is added to an fp32 product.
+struct Out {
+  void* c; int64_t ldc; int32_t bf16;
+  const float* base; int64_t ld_base;
+  int64_t M, N;
+};
+
+// The loads of 16 columns have landed.  The registers pass through the statement, so that nothing that reads them can move above it.
+__device__ __forceinline__ void tmem_ld_wait(uint32_t (&v)[16]) {
+  asm volatile("tcgen05.wait::ld.sync.aligned;"
+               : "+r"(v[0]), "+r"(v[1]), "+r"(v[2]), "+r"(v[3]), "+r"(v[4]), "+r"(v[5]), "+r"(v[6]), "+r"(v[7]), "+r"(v[8]), "+r"(v[9]),
+                 "+r"(v[10]), "+r"(v[11]), "+r"(v[12]), "+r"(v[13]), "+r"(v[14]), "+r"(v[15])
+               :: "memory");
+}
+
+// acc += f * D for COLS columns of tensor memory from `at` on, two columns per register pair; the next 16 columns load while the
+// ones before are added.  release() runs once all of them are in registers.
+template <int COLS, typename Release>
+__device__ __forceinline__ void drain(uint32_t at, uint64_t (&acc)[COLS / 2], float f, Release release) {
+  uint32_t d[2][16];
+  const uint64_t ff = pack2(__float_as_uint(f), __float_as_uint(f));
+  tmem_ld16(at, d[0]);
+  tmem_ld_wait(d[0]);
+#pragma unroll
+  for (int c = 0; c < COLS / 16; c++) {
+    if (c + 1 < COLS / 16) tmem_ld16(at + (c + 1) * 16, d[(c + 1) & 1]);
+    else release();
+#pragma unroll
+    for (int j = 0; j < 16; j += 2) acc[c * 8 + j / 2] = fma2(ff, pack2(d[c & 1][j], d[c & 1][j + 1]), acc[c * 8 + j / 2]);
+    if (c + 1 < COLS / 16) tmem_ld_wait(d[(c + 1) & 1]);
+  }
+}
+
+// Four consecutive outputs (column n a multiple of four) to their row, as the row's end allows.
+__device__ __forceinline__ void store_out4(const Out& o, int64_t m, int64_t n, float4 v) {
+  if (m >= o.M || n >= o.N) return;
+  const bool whole = n + 4 <= o.N;
+  if (o.bf16) {
+    __nv_bfloat16* p = static_cast<__nv_bfloat16*>(o.c) + m * o.ldc + n;
+    if (whole) {
+      const __nv_bfloat162 a = __floats2bfloat162_rn(v.x, v.y), b = __floats2bfloat162_rn(v.z, v.w);
+      *reinterpret_cast<uint2*>(p) = make_uint2(*reinterpret_cast<const uint32_t*>(&a), *reinterpret_cast<const uint32_t*>(&b));
+      return;
+    }
+    const float e[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int i = 0; i < 3; i++)
+      if (n + i < o.N) p[i] = __float2bfloat16_rn(e[i]);
+    return;
+  }
+  float* p = static_cast<float*>(o.c) + m * o.ldc + n;
+  if (o.base) {
+    const float* b = o.base + m * o.ld_base + n;
+    if (whole) {
+      const uint4 q = load16(b);
+      v.x += __uint_as_float(q.x); v.y += __uint_as_float(q.y); v.z += __uint_as_float(q.z); v.w += __uint_as_float(q.w);
+    } else {
+      v.x += loadf(b);
+      if (n + 1 < o.N) v.y += loadf(b + 1);
+      if (n + 2 < o.N) v.z += loadf(b + 2);
+    }
+  }
+  if (whole) { *reinterpret_cast<float4*>(p) = v; return; }
+  p[0] = v.x;
+  if (n + 1 < o.N) p[1] = v.y;
+  if (n + 2 < o.N) p[2] = v.z;
+}
+
+// A warp's 32 rows x COLS columns (row m0 + lane in this lane's registers) to memory, 32 columns at a time through 4 KB of shared
+// memory: lanes write their own rows and read four rows of 128 bytes, so that every store instruction fills whole lines (fp32; half
+// lines in bf16).  Pieces of 16 bytes lie at piece ^ (row % 8): no bank conflicts either way.
+template <int COLS>
+__device__ __forceinline__ void store_tile(const Out& o, unsigned char* stage, const uint64_t (&acc)[COLS / 2], int64_t m0, int64_t n0, int lane) {
+#pragma unroll
+  for (int c = 0; c < COLS / 32; c++) {
+    __syncwarp();                                       // the chunk before has been read
+#pragma unroll
+    for (int p = 0; p < 8; p++) {
+      float v[4];
+      unpack2(acc[c * 16 + 2 * p], v[0], v[1]);
+      unpack2(acc[c * 16 + 2 * p + 1], v[2], v[3]);
+      *reinterpret_cast<float4*>(swz(stage, lane, p)) = make_float4(v[0], v[1], v[2], v[3]);
+    }
+    __syncwarp();
+#pragma unroll
+    for (int i = 0; i < 8; i++) {
+      const int row = i * 4 + lane / 8, piece = lane % 8;
+      store_out4(o, m0 + row, n0 + c * 32 + piece * 4, *reinterpret_cast<const float4*>(swz(stage, row, piece)));
+    }
+  }
+}
+
+// ---- tiles shared by several CTAs of a cluster
+// The 16-byte piece u of a row of TN fp32 partial sums.
+template <int TN>
+__device__ __forceinline__ int part_offset(int row, int u) { return row * (TN * 4) + ((u ^ (row & 7)) << 4); }
+
+template <int TN, int COLS>
+__device__ __forceinline__ void stage_part(unsigned char* base, const uint64_t (&acc)[COLS / 2], int row, int col0) {
+#pragma unroll
+  for (int p = 0; p < COLS / 4; p++) {
+    float v[4];
+    unpack2(acc[2 * p], v[0], v[1]);
+    unpack2(acc[2 * p + 1], v[2], v[3]);
+    *reinterpret_cast<float4*>(base + part_offset<TN>(row, col0 / 4 + p)) = make_float4(v[0], v[1], v[2], v[3]);
+  }
+}
+__device__ __forceinline__ float4 ld_cluster16(uint32_t addr) {
+  float4 v;
+  asm volatile("ld.shared::cluster.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr));
+  return v;
+}
+// This CTA's share (part `mine` of `parts`) of the 128 rows of a tile whose partial sums lie in the CTAs `rank0`, `rank0` + 2, ...
+template <int TN, int MOST>
+__device__ __forceinline__ void finish_parts(const Out& o, unsigned char* base, int mine, int parts, uint32_t rank0, int64_t m0, int64_t n0, int tid,
+                                             int threads) {
+  const int r0 = mine * TM / parts, r1 = (mine + 1) * TM / parts;
+  for (int i = tid; i < (r1 - r0) * (TN / 4); i += threads) {
+    const int row = r0 + i / (TN / 4), u = i % (TN / 4);
+    if (m0 + row >= o.M || n0 + 4 * u >= o.N) continue;
+    const uint32_t at = smem_u32(base + part_offset<TN>(row, u));
+    float4 v[MOST];
+#pragma unroll
+    for (int q = 0; q < MOST; q++)
+      if (q < parts) v[q] = ld_cluster16(mapa_rank(at, rank0 + 2 * q));
+    float4 sum = v[0];
+#pragma unroll
+    for (int q = 1; q < MOST; q++)
+      if (q < parts) { sum.x += v[q].x; sum.y += v[q].y; sum.z += v[q].z; sum.w += v[q].w; }
+    store_out4(o, m0 + row, n0 + 4 * u, sum);
+  }
+}
+
+// Output tiles are walked in blocks of eight rows of tiles, column by column, so that the tiles in flight at one time cover about as
+// many rows of one operand as of the other (fewest bytes read for the products of a wave).
+__device__ __forceinline__ void tile_at(int64_t i, int64_t tiles_m, int64_t tiles_n, int64_t* tm, int64_t* tn) {
+  constexpr int64_t kRows = 8;
+  const int64_t block = i / (kRows * tiles_n), in = i - block * (kRows * tiles_n);
+  const int64_t rows = tiles_m - block * kRows < kRows ? tiles_m - block * kRows : kRows;
+  *tn = in / rows;
+  *tm = block * kRows + (in - *tn * rows);
+}
+
+}  // namespace fp8
+}  // namespace hbmm

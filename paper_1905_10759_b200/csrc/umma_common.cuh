@@ -261,6 +261,13 @@ __device__ __forceinline__ void umma_bf16_pair(uint32_t d_tmem, uint64_t a_desc,
       "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}"
       ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate) : "memory");
 }
+// The same for e4m3 operands, 256 x N x 32.
+__device__ __forceinline__ void umma_f8_pair(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::2.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}"
+      ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate) : "memory");
+}
 // Arrives, once the pair's MMAs issued so far have completed, on the barrier at this address in every CTA of the mask.
 __device__ __forceinline__ void umma_commit_pair_mc(uint32_t bar, uint16_t cta_mask) {
   asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;"
@@ -311,6 +318,8 @@ __host__ __device__ constexpr uint32_t instr_desc_pair(int n, uint32_t ab_format
   return (1u << 4) | (ab_format << 7) | (ab_format << 10) | (static_cast<uint32_t>(n >> 3) << 17) |
          (static_cast<uint32_t>((2 * TM) >> 4) << 24);
 }
+// Added to an instruction descriptor: that operand is MN-major (its contraction index is the outer one in memory).
+constexpr uint32_t kTransposeA = 1u << 15, kTransposeB = 1u << 16;
 constexpr uint32_t kFmtE4M3 = 0, kFmtBF16 = 1;   // kind::f8f6f4 / kind::f16 operand codes
 constexpr uint32_t kFmtF16 = 0;                  // kind::f16 with fp16 operands
 
