@@ -2,19 +2,27 @@
 //
 //   C[m,n] = sum_g (sA[m,g] sW[n/128,g]) D_g[m,n],   D_g[m,n] = sum_{k in group g} A[m,k] W[n,k]
 //
-// A pair of CTAs forms D_g of a 256 x 256 tile with four 256 x 256 x 32 MMAs (kind::f8f6f4, cta_group::2) into one of two
-// accumulators in tensor memory; eight epilogue warps per CTA add it, times the two scales, to fp32 registers (128 columns of one
-// row per thread: both scales are one number per thread and group, so the scaling is one fma per output, two per instruction),
-// while the tensor cores fill the other accumulator.  512 clk of MMA against 256 of fma and 256 of tensor-memory reads per group.
-// The scales are fp32 numbers of any value: they are applied to fp32 sums, no power of two is assumed.
+// A pair of CTAs takes a 256 x 256 tile (cta_group::2, 256 x N x 32 MMAs); how it sums the groups goes by their scales, four groups
+// (a step) at a time:
+//   * all of them powers of two (what hbmm_fp8_quantize writes): the tensor cores apply them (kind::mxf8f6f4, block scales: a UE8M0
+//     byte per row and 32 elements, here the same byte for the four instructions of a group) and the whole walk along K is one
+//     accumulation in tensor memory, 256 columns;
+//   * otherwise each group's dot products go to one of three units of 128 columns, and the epilogue adds them, times the two scales,
+//     to fp32 registers.  The accumulation in tensor memory is left where it stands and taken first.
+// The second way is bound by the round trip from the MMA's completion to the epilogue and back (8192^3: 1.08 ms when every product
+// went that way); the first by the tensor cores' power (0.40 ms, 2.75 PFLOP/s; its MMAs alone 0.29 ms).
 //
 // C = A^ W^ (the input gradient; the contraction runs along the rows of W) reads the same W: its tiles arrive as 128 rows of the
 // contraction x 128 columns and enter the MMA as an MN-major operand.  Nothing is transposed in memory.
 //
 // Per CTA and group 16 KB of A (its own 128 rows) and 16 KB of W (its half of the 256 columns) arrive by tensor copies (128-byte
 // swizzle, zeros outside the matrices, so no edge needs a case of its own); six stages in flight.
-//   warps 0-7 : epilogue (TMEM lanes 32 * (w % 4).., columns 128 * (w / 4)..)
-//   warp  8   : one thread issues this CTA's copies;  warp 9 : TMEM allocation, and in the first CTA the MMA-issuing thread (10, 11 hand over registers)
+//   warps 0-7   : epilogue (TMEM lanes 32 * (w % 4)..; columns 64 h .. and 128 + 64 h .. with h = w / 4)
+//   warp  8     : one thread issues this CTA's copies;  warp 9 : TMEM allocation, and in the first CTA the MMA-issuing thread
+//   warp  10    : copies each step's scales to shared memory, up to eight steps ahead (11 hands over registers)
+//   warps 12-15 : scouts: look the scales over and write their exponents to tensor memory
+// What both CTAs have to know (their scales' kind) goes as asynchronous stores that complete on the barrier the readers wait at; the
+// arrivals across the pair release nothing but reads.  (Store and releasing arrival: 2600 clk beside the copies, 0.53 ms.)
 // Products of few tiles: a cluster of two or four pairs shares each tile in equal parts of K (fp8_tile.cuh).
 #include <cuda_bf16.h>
 #include "fp8_tile.cuh"
@@ -27,15 +35,25 @@ namespace {
 
 using namespace fp8;
 
-constexpr int TN = 256, COLS = TN / 2;         // columns of a pair's tile; of an epilogue warp
-constexpr int kThreads = 12 * 32, kLoaderWarp = 8, kMmaWarp = 9, kEpilogueWarps = 8;
-constexpr int kRegsEpilogue = 208, kRegsOthers = 80;     // 256 x 208 + 128 x 80 of the 384 x 168 registers at launch
+constexpr int TN = 256;                        // columns of a pair's tile
+constexpr int kThreads = 16 * 32, kEpilogueWarps = 8, kLoaderWarp = 8, kMmaWarp = 9, kScaleWarp = 10, kScoutWarp = 12;
+constexpr int kRegsEpilogue = 200, kRegsIssue = 56, kRegsScout = 56;      // 256 x 200 + 128 x 56 + 128 x 56 = 64 K registers
 constexpr int kTile = 128 * 128;               // bytes of an operand's part of a stage
 constexpr int STAGE = 2 * kTile, STAGES = 6;
-constexpr int OFF_A = 0, OFF_B = STAGES * kTile, OFF_OUT = STAGES * STAGE, OFF_BAR = OFF_OUT + kEpilogueWarps * 4096;
-constexpr int kBytes = OFF_BAR + (2 * STAGES + 5) * 8 + 16;
+// A step is four groups: its scales arrive together, beside the stages.  Shared memory of a slot: 128 rows x 4 scales of A, then W's.
+constexpr int kStep = 4, kSlots = 8, kScalesA = 128 * kStep * 4, kSlotBytes = kScalesA + 128;
+// Tensor memory: three units of 128 columns for partial sums (a whole accumulator takes the first two), then the factors of each
+// slot, 16 columns (4 of A, 8 of W).
+// A whole accumulator takes 16 steps (8192 elements) at most: the tensor cores' fp32 sums truncate, and the relative error of a result
+// grows with their number (256 x 256 outputs of K = 4096 / 8192: 7e-8 / 1.2e-7, 6e-8 / 7.5e-8 with a sum per group).
+constexpr int kChunk = 16;
+constexpr int kUnit = 128, kUnits = 3, kFactorCols = 384, kFactorSlot = 16;
+constexpr int OFF_A = 0, OFF_B = STAGES * kTile, OFF_OUT = STAGES * STAGE, OFF_SCALES = OFF_OUT + kEpilogueWarps * kStoreBytes;
+constexpr int OFF_BAR = OFF_SCALES + kSlots * kSlotBytes;
+constexpr int kBars = 2 * STAGES + 2 * kUnits + 2 + 3 * kSlots + 1;
+constexpr int OFF_FLAGS = OFF_BAR + kBars * 8, kBytes = OFF_FLAGS + kSlots * 8 + 16;
 constexpr int kMostParts = 4;                  // pairs that share a tile
-static_assert(kBytes <= 227 * 1024 && TM * TN * 4 <= STAGES * STAGE, "shared memory");
+static_assert(kBytes <= 227 * 1024 && TM * TN * 4 <= STAGES * STAGE && kFactorCols + kSlots * kFactorSlot <= 512, "shared and tensor memory");
 
 struct Args {
   const float* a_s; int64_t ld_as;
@@ -45,16 +63,31 @@ struct Args {
   int32_t parts;                               // pairs (of one cluster) that share a tile
 };
 
+// A normal power of two: what the tensor cores' own factors can be.
+__device__ __forceinline__ bool is_factor(uint32_t bits) { return (bits & 0x807FFFFFu) == 0 && bits - 0x00800000u < 0x7F000000u; }
+
+// The scale of the tile's block b (0, 1) of columns in the step's group j.
+template <bool TRANS>
+__device__ __forceinline__ float w_scale(const unsigned char* at, int b, int j) {
+  return *reinterpret_cast<const float*>(at + (TRANS ? j * 2 + b : b * 4 + j) * 4);
+}
+
 template <bool TRANS>
 __global__ void __launch_bounds__(kThreads, 1)
 fp8_gemm_kernel(const Args g, const __grid_constant__ CUtensorMap a_map, const __grid_constant__ CUtensorMap w_map) {
   extern __shared__ __align__(1024) unsigned char smem[];
   uint64_t* full = reinterpret_cast<uint64_t*>(smem + OFF_BAR);
   uint64_t* empty = full + STAGES;
-  uint64_t* tfull = empty + STAGES;
-  uint64_t* tempty = tfull + 2;
-  uint64_t* drained = tempty + 2;
-  uint32_t* tmem_base_ptr = reinterpret_cast<uint32_t*>(drained + 1);
+  uint64_t* ufull = empty + STAGES;            // units of partial sums
+  uint64_t* uempty = ufull + kUnits;
+  uint64_t* xfull = uempty + kUnits;           // the whole accumulator
+  uint64_t* xempty = xfull + 1;
+  uint64_t* scales = xempty + 1;               // a step's scales are in this CTA's shared memory
+  uint64_t* sfull = scales + kSlots;           // its factors are in both CTAs' tensor memory, and how it is summed is known
+  uint64_t* sempty = sfull + kSlots;           // its slot is free in both CTAs
+  uint64_t* drained = sempty + kSlots;
+  uint32_t* flags = reinterpret_cast<uint32_t*>(smem + OFF_FLAGS);             // [kSlots][CTA of the pair]: the scales are factors
+  uint32_t* tmem_base_ptr = flags + kSlots * 2;
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_base_ptr + 1);
 
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -63,7 +96,9 @@ fp8_gemm_kernel(const Args g, const __grid_constant__ CUtensorMap a_map, const _
   const int part = static_cast<int>(rank >> 1);
   // the pair's walk: tiles of its own, or one tile's groups [g0, g1) of `parts`
   const int64_t walker = blockIdx.x / (2 * g.parts), walkers = gridDim.x / (2 * g.parts);
-  const int g0 = static_cast<int>(static_cast<int64_t>(part) * g.groups / g.parts), g1 = static_cast<int>(static_cast<int64_t>(part + 1) * g.groups / g.parts);
+  const int steps = (g.groups + kStep - 1) / kStep;
+  const int g0 = static_cast<int>(static_cast<int64_t>(part) * steps / g.parts) * kStep;
+  const int g_end = static_cast<int>(static_cast<int64_t>(part + 1) * steps / g.parts) * kStep, g1 = g_end < g.groups ? g_end : g.groups;
 
   pdl_launch_dependents();
   if (tid == 0) {
@@ -71,7 +106,14 @@ fp8_gemm_kernel(const Args g, const __grid_constant__ CUtensorMap a_map, const _
       mbar_init(&full[s], 1);           // first CTA: its loader's expect_tx arrival; the copies of both CTAs complete the bytes
       mbar_init(&empty[s], 1);          // MMA commit (to both CTAs)
     }
-    for (int b = 0; b < 2; b++) { mbar_init(&tfull[b], 1); mbar_init(&tempty[b], 2 * kEpilogueWarps); }
+    for (int u = 0; u < kUnits; u++) { mbar_init(&ufull[u], 1); mbar_init(&uempty[u], kEpilogueWarps); }    // one warpgroup of each CTA
+    mbar_init(xfull, 1);
+    mbar_init(xempty, 2 * kEpilogueWarps);
+    for (int f = 0; f < kSlots; f++) {
+      mbar_init(&scales[f], 32);                            // the scale loader's lanes
+      mbar_init(&sfull[f], 8);                              // scout warps of both CTAs
+      mbar_init(&sempty[f], 2 * kEpilogueWarps + 1);        // epilogue warps of both CTAs, MMA commit
+    }
     mbar_init(drained, 1);
     *abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -86,8 +128,14 @@ fp8_gemm_kernel(const Args g, const __grid_constant__ CUtensorMap a_map, const _
   cluster_sync_all();                  // every CTA's barriers exist before another signals them
   tc_fence_after();
   const uint32_t tmem_base = *tmem_base_ptr;
+  const Waiter wait{g_spin_limit, abort_flag};
+  const auto are_factors = [&](uint32_t f) {           // behind sfull
+    const volatile uint32_t* v = flags + f * 2;
+    return (v[0] & v[1]) != 0;
+  };
 
-  if (warp >= kEpilogueWarps) reg_dec<kRegsOthers>();
+  if (warp >= kScoutWarp) reg_dec<kRegsScout>();
+  else if (warp >= kEpilogueWarps) reg_dec<kRegsIssue>();
   if (warp == kLoaderWarp) {
     // =========================== loader (both CTAs) ===========================
     if (elect_one()) {
@@ -103,7 +151,7 @@ fp8_gemm_kernel(const Args g, const __grid_constant__ CUtensorMap a_map, const _
         tile_at(tile, tiles_m, tiles_n, &tm, &tn);
         const int32_t a_row = static_cast<int32_t>(tm * 2 * TM + half * TM), w_at = static_cast<int32_t>(tn * TN + half * (TN / 2));
         for (int kb = g0; kb < g1; kb++) {
-          if (round > 0 && !mbar_wait(&empty[s], (round & 1) ^ 1, abort_flag, 1)) { ok = false; break; }
+          if (round > 0 && !wait(smem_u32(&empty[s]), (round & 1) ^ 1, 1)) { ok = false; break; }
           if (half == 0) mbar_arrive_expect_tx(&full[s], 2 * STAGE);
           const uint32_t bar = full0 + s * 8;
           tma_load_2d_pair(smem + OFF_A + s * kTile, &a_map, kb * kGroup, a_row, bar);
@@ -128,97 +176,262 @@ fp8_gemm_kernel(const Args g, const __grid_constant__ CUtensorMap a_map, const _
       }
     }
     __syncwarp();
+  } else if (warp == kScaleWarp) {
+    // =========================== scale loader (both CTAs) ===========================
+    // As far ahead of the stages as there are slots.  16 bytes of every row: by lanes, as a tensor copy takes such short rows one by
+    // one and holds up the stages behind it.
+    uint32_t f = 0, f_par = 1;                           // the first round waits for nobody
+    bool ok = true;
+    for (int64_t tile = walker; tile < n_tiles && ok; tile += walkers) {
+      int64_t tm, tn;
+      tile_at(tile, tiles_m, tiles_n, &tm, &tn);
+      const int64_t m0 = tm * 2 * TM + half * TM, rows = g.out.M - m0;
+      for (int kb = g0; kb < g1; kb += kStep) {
+        if (!wait(smem_u32(&sempty[f]), f_par, 8)) { ok = false; break; }
+        const uint32_t slot = smem_u32(smem + OFF_SCALES + f * kSlotBytes);
+        const int bytes = 4 * (g1 - kb < kStep ? g1 - kb : kStep);
+#pragma unroll
+        for (int c = 0; c < 4; c++) {
+          const int row = 32 * c + lane;
+          const bool in = row < rows;
+          cp_async16(slot + row * 16, g.a_s + (in ? (m0 + row) * g.ld_as + kb : 0), in ? bytes : 0);
+        }
+        // W's, [block][group] or [group][block]: one by one (the two blocks need not lie in one aligned 16 bytes)
+        const int b = TRANS ? lane & 1 : lane >> 2, j = TRANS ? lane >> 1 : lane & 3;
+        if (lane < 8) {
+          const bool in = kb + j < g1 && (tn * 2 + b) * kGroup < g.out.N;
+          cp_async4(slot + kScalesA + lane * 4, g.w_s + (in ? (tn * 2 + b) * g.w_step_n + (kb + j) * g.w_step_g : 0), in ? 4 : 0);
+        }
+        cp_async_arrive(&scales[f]);
+        if (++f == kSlots) { f = 0; f_par ^= 1; }
+      }
+    }
+    cp_async_wait_all();                                 // also after an abort
+    __syncwarp();
   } else if (warp == kMmaWarp) {
     // =========================== MMA issuer (first CTA of the pair) ===========================
     if (half == 0 && elect_one()) {
-      constexpr uint32_t idesc = instr_desc_pair(TN, kFmtE4M3) | (TRANS ? kTransposeB : 0u);
+      constexpr uint32_t kMajor = TRANS ? kTransposeB : 0u;
       // 32 elements of the contraction: 32 bytes along K-major rows, 32 rows of 128 bytes of an MN-major tile
       constexpr uint32_t kStepA = 32 >> 4, kStepB = (TRANS ? 32 * 128 : 32) >> 4;
+      constexpr uint32_t kHalfB = (TRANS ? 64 : 64 * 128) >> 4;            // 64 columns further
       const uint16_t both = static_cast<uint16_t>(3u << lead);
       const uint64_t da0 = smem_desc(smem_u32(smem + OFF_A)), db0 = smem_desc(smem_u32(smem + OFF_B));
       const uint64_t da_hi = da0 & 0xFFFFFFFF00000000ull, db_hi = db0 & 0xFFFFFFFF00000000ull;
       const uint32_t da_lo = static_cast<uint32_t>(da0), db_lo = static_cast<uint32_t>(db0);
-      const uint32_t full_a = smem_u32(full), empty_a = smem_u32(empty), tfull_a = smem_u32(tfull), tempty_a = smem_u32(tempty);
-      uint32_t s = 0, full_par = 0, it = 0;
+      const uint32_t full_a = smem_u32(full), empty_a = smem_u32(empty), ufull_a = smem_u32(ufull), uempty_a = smem_u32(uempty);
+      const uint32_t sempty_a = smem_u32(sempty);
+      uint32_t s = 0, full_par = 0;            // stage
+      uint32_t u = 0, u_round = 0;             // unit of the next partial sum, and how often the ring went round
+      uint32_t x = 0;                          // whole accumulators so far
+      uint32_t f = 0, f_par = 0;               // slot of scales
       bool ok = true;
-      for (int64_t tile = walker; tile < n_tiles && ok; tile += walkers) {
-        for (int kb = g0; kb < g1; kb++, it++) {
-          const uint32_t buf = it & 1;
-          if (it >= 2 && !mbar_wait_a(tempty_a + buf * 8, ((it >> 1) & 1) ^ 1, abort_flag, 3)) { ok = false; break; }
-          if (!mbar_wait_a(full_a + s * 8, full_par, abort_flag, 2)) { ok = false; break; }
-          tc_fence_after();
-          const uint32_t a_lo = da_lo + s * (kTile >> 4), b_lo = db_lo + s * (kTile >> 4);
-#pragma unroll
-          for (uint32_t ks = 0; ks < kGroup / 32; ks++)
-            umma_f8_pair(tmem_base + buf * TN, da_hi | (a_lo + ks * kStepA), db_hi | (b_lo + ks * kStepB), idesc, ks != 0 ? 1u : 0u);
-          umma_commit_pair_mc(empty_a + s * 8, both);
-          umma_commit_pair_mc(tfull_a + buf * 8, both);
-          if (++s == STAGES) { s = 0; full_par ^= 1; }
+      // the accumulator's columns are free: the units' last partial sums and the last whole accumulator have been read
+      const auto accumulator_free = [&] {
+        if (x > 0 && !wait(smem_u32(xempty), (x & 1) ^ 1, 3)) return false;
+        for (uint32_t i = 0; i < 2; i++) {
+          const uint32_t uses = u_round + (u > i ? 1 : 0);
+          if (uses > 0 && !wait(uempty_a + i * 8, (uses & 1) ^ 1, 3)) return false;
         }
+        return true;
+      };
+      for (int64_t tile = walker; tile < n_tiles && ok; tile += walkers) {
+        int open = 0;                          // steps in the accumulator
+        const auto close = [&] {
+          umma_commit_pair_mc(smem_u32(xfull), both);
+          x++;
+          open = 0;
+        };
+        for (int kb0 = g0; kb0 < g1 && ok; kb0 += kStep) {
+          if (!wait(smem_u32(&sfull[f]), f_par, 7)) { ok = false; break; }
+          tc_fence_after();
+          const int n = g1 - kb0 < kStep ? g1 - kb0 : kStep;
+          if (are_factors(f)) {
+            if (open == 0 && !accumulator_free()) { ok = false; break; }
+            const uint32_t sa = tmem_base + kFactorCols + f * kFactorSlot;
+            uint32_t idesc = instr_desc_mx_pair(TN) | kMajor;
+            for (int j = 0; j < n; j++) {
+              if (!wait(full_a + s * 8, full_par, 2)) { ok = false; break; }
+              tc_fence_after();
+              const uint32_t a_lo = da_lo + s * (kTile >> 4), b_lo = db_lo + s * (kTile >> 4);
+#pragma unroll
+              for (uint32_t ks = 0; ks < kGroup / 32; ks++)
+                umma_mxf8_pair(tmem_base, da_hi | (a_lo + ks * kStepA), db_hi | (b_lo + ks * kStepB), idesc, sa, sa + 4,
+                               open != 0 || j != 0 || ks != 0 ? 1u : 0u);
+              umma_commit_pair_mc(empty_a + s * 8, both);
+              if (++s == STAGES) { s = 0; full_par ^= 1; }
+              idesc += instr_desc_mx_byte(1);
+            }
+            if (ok && ++open == kChunk) close();
+          } else {
+            if (open != 0) close();
+            constexpr uint32_t idesc = instr_desc_pair(kUnit, kFmtE4M3) | kMajor;
+            for (int j = 0; j < n && ok; j++) {
+              for (uint32_t h = 0; h < 2; h++) {
+                if (u < 2 && x > 0 && !wait(smem_u32(xempty), (x & 1) ^ 1, 3)) { ok = false; break; }
+                if (u_round > 0 && !wait(uempty_a + u * 8, (u_round & 1) ^ 1, 3)) { ok = false; break; }
+                if (h == 0 && !wait(full_a + s * 8, full_par, 2)) { ok = false; break; }
+                tc_fence_after();
+                const uint32_t a_lo = da_lo + s * (kTile >> 4), b_lo = db_lo + s * (kTile >> 4) + h * kHalfB;
+#pragma unroll
+                for (uint32_t ks = 0; ks < kGroup / 32; ks++)
+                  umma_f8_pair(tmem_base + u * kUnit, da_hi | (a_lo + ks * kStepA), db_hi | (b_lo + ks * kStepB), idesc, ks != 0 ? 1u : 0u);
+                umma_commit_pair_mc(ufull_a + u * 8, both);
+                if (++u == kUnits) { u = 0; u_round++; }
+              }
+              if (!ok) break;
+              umma_commit_pair_mc(empty_a + s * 8, both);
+              if (++s == STAGES) { s = 0; full_par ^= 1; }
+            }
+          }
+          if (!ok) break;
+          umma_commit_pair_mc(sempty_a + f * 8, both);
+          if (++f == kSlots) { f = 0; f_par ^= 1; }
+        }
+        if (ok && open != 0) close();
       }
       // every MMA issued so far has retired (in both CTAs) before tensor memory is released -- also after an abort
       umma_commit_pair(smem_u32(drained));
-      if (!mbar_wait_quiet(drained, 0, g_spin_limit < kDrainPolls ? kDrainPolls : g_spin_limit)) {
+      if (!mbar_wait_quiet(drained, 0, wait.limit < kDrainPolls ? kDrainPolls : wait.limit)) {
         atomicCAS(&g_error_word, 0, 4);
         *abort_flag = 1;
       }
     }
     __syncwarp();
+  } else if (warp >= kScoutWarp) {
+    // =========================== scouts (both CTAs) ===========================
+    // A step's scales as they arrive: whether all of them are powers of two, and their exponents into tensor memory.  (Nobody loads
+    // them when they are needed: a load waits behind the copies in flight, 2 to 3 us for the 192 KB of an SM's stages.)
+    const int quarter = warp - kScoutWarp;
+    const uint32_t factor_at = tmem_base + (static_cast<uint32_t>(quarter * 32) << 16) + kFactorCols;
+    uint32_t f = 0, f_par = 0;
+    bool ok = true;
+    for (int64_t tile = walker; tile < n_tiles && ok; tile += walkers) {
+      int64_t tm, tn;
+      tile_at(tile, tiles_m, tiles_n, &tm, &tn);
+      const int64_t rows = g.out.M - (tm * 2 * TM + half * TM);            // of this CTA's half tile on
+      const bool second = tn * TN + kGroup < g.out.N;                      // the tile has a second block of columns
+      for (int kb = g0; kb < g1; kb += kStep) {
+        if (!wait(smem_u32(&scales[f]), f_par, 8)) { ok = false; break; }
+        const unsigned char* slot = smem + OFF_SCALES + f * kSlotBytes;
+        const int n = g1 - kb < kStep ? g1 - kb : kStep;
+        constexpr uint32_t kOne = 0x3F800000u;
+        bool good = true;
+        uint32_t a[4], w[2] = {0, 0};
+#pragma unroll
+        for (int c = 0; c < 4; c++) {                                      // rows 32 c + lane
+          const uint4 v = *reinterpret_cast<const uint4*>(slot + (32 * c + lane) * 16);
+          const bool in = 32 * c + lane < rows;
+          const uint32_t e[4] = {in ? v.x : kOne, in && n > 1 ? v.y : kOne, in && n > 2 ? v.z : kOne, in && n > 3 ? v.w : kOne};
+          a[c] = 0;
+#pragma unroll
+          for (int j = 0; j < kStep; j++) { good &= is_factor(e[j]); a[c] |= (e[j] >> 23) << (8 * j); }
+        }
+#pragma unroll
+        for (int b = 0; b < 2; b++)
+#pragma unroll
+          for (int j = 0; j < kStep; j++) {
+            const uint32_t e = j < n && (b == 0 || second) ? __float_as_uint(w_scale<TRANS>(slot + kScalesA, b, j)) : kOne;
+            good &= is_factor(e);
+            w[b] |= (e >> 23 & 0xFFu) << (8 * j);
+          }
+        good = __all_sync(0xffffffffu, good);
+        tc_fence_after();                                                  // the slot's last MMAs, through the scale loader's wait
+        const uint32_t at = factor_at + f * kFactorSlot, w0[4] = {w[0], w[0], w[0], w[0]}, w1[4] = {w[1], w[1], w[1], w[1]};
+        tmem_st4(at, a);
+        tmem_st4(at + 4, w0);
+        tmem_st4(at + 8, w1);
+        tmem_st_wait();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) {
+          const uint32_t bar = smem_u32(&sfull[f]);
+          if (quarter == 0) {                              // both CTAs' verdicts to both CTAs
+            for (uint32_t c = 0; c < 2; c++)
+              st_async_u32(mapa_rank(smem_u32(flags + f * 2 + half), lead + c), good ? 1u : 0u, mapa_rank(bar, lead + c));
+            mbar_arrive_expect_tx(&sfull[f], 8);
+          } else {
+            mbar_arrive(&sfull[f]);
+          }
+          mbar_arrive_cluster_read(mapa_rank(bar, rank ^ 1u));
+        }
+        __syncwarp();
+        if (++f == kSlots) { f = 0; f_par ^= 1; }
+      }
+    }
   } else if (warp < kEpilogueWarps) {
     // =========================== epilogue (both CTAs) ===========================
     reg_inc<kRegsEpilogue>();
-    const int row = (warp & 3) * 32 + lane, col0 = (warp >> 2) * COLS;
-    const uint32_t tmem_at = tmem_base + (static_cast<uint32_t>((warp & 3) * 32) << 16) + col0;
-    const uint32_t tempty0 = mapa_rank(smem_u32(tempty), lead);
-    unsigned char* stage = smem + OFF_OUT + warp * 4096;
-    constexpr int AHEAD = 4;                     // groups whose scales are loaded at a time, while those before are used
-    float na[AHEAD], nw[AHEAD];
-    int64_t tm = 0, tn = 0;
-    const auto fetch = [&](int64_t tile, int kb) {
-      if (tile >= n_tiles) return;
-      tile_at(tile, tiles_m, tiles_n, &tm, &tn);
-      const int64_t m = tm * 2 * TM + half * TM + row, n = tn * TN + col0;
-      const float* ap = g.a_s + m * g.ld_as;
-      const float* wp = g.w_s + n / kGroup * g.w_step_n;
-#pragma unroll
-      for (int j = 0; j < AHEAD; j++) {
-        const bool in = kb + j < g1 && m < g.out.M && n < g.out.N;
-        na[j] = in ? loadf(ap + kb + j) : 0.0f;
-        nw[j] = in ? loadf(wp + (kb + j) * g.w_step_g) : 0.0f;
-      }
-    };
-    uint32_t it = 0;
+    const int row = (warp & 3) * 32 + lane;
+    const uint32_t h = warp >> 2;                // columns 64 h .. and 128 + 64 h .. of the tile
+    const uint32_t tmem_at = tmem_base + (static_cast<uint32_t>((warp & 3) * 32) << 16);
+    const uint32_t uempty0 = mapa_rank(smem_u32(uempty), lead), xempty0 = mapa_rank(smem_u32(xempty), lead);
+    unsigned char* stage = smem + OFF_OUT + warp * kStoreBytes;
+    uint32_t u = h, u_par = 0;                   // unit of this warpgroup's next partial sum: every second one is its own
+    uint32_t x_par = 0, f = 0, f_par = 0;
+    uint64_t acc[kRun];
     bool ok = true;
-    fetch(walker, g0);
     for (int64_t tile = walker; tile < n_tiles && ok; tile += walkers) {
-      uint64_t acc[COLS / 2];
-#pragma unroll
-      for (int j = 0; j < COLS / 2; j++) acc[j] = 0ull;
+      int64_t tm, tn;
+      tile_at(tile, tiles_m, tiles_n, &tm, &tn);
       const int64_t m0 = tm * 2 * TM + half * TM, n0 = tn * TN;
-      for (int kb0 = g0; kb0 < g1 && ok; kb0 += AHEAD) {
-        float fa[AHEAD], fw[AHEAD];
 #pragma unroll
-        for (int j = 0; j < AHEAD; j++) { fa[j] = na[j]; fw[j] = nw[j]; }
-        if (kb0 + AHEAD < g1) fetch(tile, kb0 + AHEAD);
-        else fetch(tile + walkers, g0);
-        const int n = g1 - kb0 < AHEAD ? g1 - kb0 : AHEAD;
+      for (int j = 0; j < kRun; j++) acc[j] = 0ull;
+      int open = 0;
+      const auto take_accumulator = [&] {
+        if (!wait(smem_u32(xfull), x_par, 5)) return false;
+        tc_fence_after();
+        drain(tmem_at + 64 * h, tmem_at + 128 + 64 * h, acc, 1.0f, 1.0f, [&] {
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive_cluster_read(xempty0);
+        });
+        x_par ^= 1;
+        open = 0;
+        return true;
+      };
+      // `open` counts as the MMA issuer's does; a full accumulator is taken at the next step or at the tile's end
+      for (int kb0 = g0; kb0 < g1 && ok; kb0 += kStep) {
+        if (!wait(smem_u32(&sfull[f]), f_par, 6)) { ok = false; break; }
+        const bool factors = are_factors(f);
+        const int n = g1 - kb0 < kStep ? g1 - kb0 : kStep;
+        if (open != 0 && (!factors || open == kChunk) && !take_accumulator()) { ok = false; break; }
+        if (factors) {
+          open++;
+        } else {
+          const unsigned char* slot = smem + OFF_SCALES + f * kSlotBytes;
 #pragma unroll 1
-        for (int j = 0; j < n; j++, it++) {
-          const uint32_t buf = it & 1;
-          const float f = j == 0 ? fa[0] * fw[0] : j == 1 ? fa[1] * fw[1] : j == 2 ? fa[2] * fw[2] : fa[3] * fw[3];
-          if (!mbar_wait(&tfull[buf], (it >> 1) & 1, abort_flag, 5)) { ok = false; break; }
-          tc_fence_after();
-          drain<COLS>(tmem_at + buf * TN, acc, f, [&] {
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0) mbar_arrive_cluster(tempty0 + buf * 8);
-          });
+          for (int j = 0; j < n; j++) {
+            const float sa = *reinterpret_cast<const float*>(slot + row * 16 + j * 4);
+            const float f0 = sa * w_scale<TRANS>(slot + kScalesA, 0, j), f1 = sa * w_scale<TRANS>(slot + kScalesA, 1, j);
+            if (!wait(smem_u32(&ufull[u]), u_par, 5)) { ok = false; break; }
+            tc_fence_after();
+            drain(tmem_at + u * kUnit, tmem_at + u * kUnit + 64, acc, f0, f1, [&] {
+              tc_fence_before();
+              __syncwarp();
+              if (lane == 0) mbar_arrive_cluster_read(uempty0 + u * 8);
+            });
+            u += 2;
+            if (u >= kUnits) { u -= kUnits; u_par ^= 1; }
+          }
+          if (!ok) break;
         }
+        __syncwarp();
+        if (lane == 0) {
+          mbar_arrive_cluster_read(mapa_rank(smem_u32(&sempty[f]), lead));
+          mbar_arrive_cluster_read(mapa_rank(smem_u32(&sempty[f]), lead + 1));
+        }
+        if (++f == kSlots) { f = 0; f_par ^= 1; }
       }
+      if (ok && open != 0 && !take_accumulator()) ok = false;
       if (!ok) break;
-      if (g.parts == 1) store_tile<COLS>(g.out, stage, acc, m0 + (warp & 3) * 32, n0 + col0, lane);
-      // every copy of this CTA's only tile has been read: its partial sums take the stages' place
-      else stage_part<TN, COLS>(smem, acc, row, col0);
+      if (g.parts == 1) store_tile(g.out, stage, acc, m0 + (warp & 3) * 32, n0 + 64 * h, n0 + 128 + 64 * h, lane);
+    }
+    if (g.parts > 1) {
+      // The partial sums of this CTA's only tile take the stages' place, once both warpgroups have seen their last unit: the MMAs
+      // of the other one's may still read the last stage.
+      asm volatile("bar.sync 1, 256;" ::: "memory");
+      if (ok) stage_part<TN>(smem, acc, row, 64 * h, 128 + 64 * h);
     }
   }
 
@@ -233,7 +446,8 @@ fp8_gemm_kernel(const Args g, const __grid_constant__ CUtensorMap a_map, const _
     __syncwarp();
   }
   // No CTA may leave while another can still reach into it (the MMAs read the second CTA's shared memory and write its tensor
-  // memory; copies and epilogue warps signal the first one's barriers; partial sums are read by the whole cluster).
+  // memory; copies, scouts and epilogue warps signal barriers of both; partial sums are read by the whole cluster).
+  __syncwarp();
   tc_fence_before();
   __syncthreads();
   cluster_sync_all();
@@ -243,7 +457,7 @@ fp8_gemm_kernel(const Args g, const __grid_constant__ CUtensorMap a_map, const _
   }
 }
 
-// Byte matrix [rows, cols] in boxes of 128 rows x 128 bytes.
+// Byte matrix [rows, cols] in boxes of 128 rows x 128 bytes; zeros outside.
 bool make_map(const Fp8View& v, CUtensorMap* map) {
   EncodeTiledFn fn = encode_tiled_fn();
   if (!fn) return false;
@@ -254,10 +468,11 @@ bool make_map(const Fp8View& v, CUtensorMap* map) {
             CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-// Pairs per tile: as many (1, 2, 4) as keep every cluster resident, two groups at least for each.
+// Pairs per tile: as many (1, 2, 4) as the machine holds at once, a step at least for each.
 int choose_parts(int64_t tiles, int64_t pairs, int groups) {
+  const int steps = (groups + kStep - 1) / kStep;
   int parts = 1;
-  while (parts < kMostParts && tiles * parts * 2 <= pairs && groups >= parts * 2 * 2) parts *= 2;
+  while (parts < kMostParts && tiles * parts * 2 <= pairs && steps >= parts * 2) parts *= 2;
   return parts;
 }
 

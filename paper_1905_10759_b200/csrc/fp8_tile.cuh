@@ -26,21 +26,24 @@ __device__ __forceinline__ void tmem_ld_wait(uint32_t (&v)[16]) {
                :: "memory");
 }
 
-// acc += f * D for COLS columns of tensor memory from `at` on, two columns per register pair; the next 16 columns load while the
-// ones before are added.  release() runs once all of them are in registers.
-template <int COLS, typename Release>
-__device__ __forceinline__ void drain(uint32_t at, uint64_t (&acc)[COLS / 2], float f, Release release) {
+// A thread's accumulators are two runs of 64 columns of its row, two columns per register pair.
+constexpr int kRun = 64;
+
+// acc += f0 * D for the run at at0 and f1 * D for the run at at1; 16 columns load while the ones before are added.  release() runs
+// once all of them are in registers.
+template <typename Release>
+__device__ __forceinline__ void drain(uint32_t at0, uint32_t at1, uint64_t (&acc)[kRun], float f0, float f1, Release release) {
   uint32_t d[2][16];
-  const uint64_t ff = pack2(__float_as_uint(f), __float_as_uint(f));
-  tmem_ld16(at, d[0]);
+  const uint64_t ff[2] = {pack2(__float_as_uint(f0), __float_as_uint(f0)), pack2(__float_as_uint(f1), __float_as_uint(f1))};
+  tmem_ld16(at0, d[0]);
   tmem_ld_wait(d[0]);
 #pragma unroll
-  for (int c = 0; c < COLS / 16; c++) {
-    if (c + 1 < COLS / 16) tmem_ld16(at + (c + 1) * 16, d[(c + 1) & 1]);
+  for (int c = 0; c < 8; c++) {
+    if (c + 1 < 8) tmem_ld16((c + 1 < 4 ? at0 : at1) + ((c + 1) % 4) * 16, d[(c + 1) & 1]);
     else release();
 #pragma unroll
-    for (int j = 0; j < 16; j += 2) acc[c * 8 + j / 2] = fma2(ff, pack2(d[c & 1][j], d[c & 1][j + 1]), acc[c * 8 + j / 2]);
-    if (c + 1 < COLS / 16) tmem_ld_wait(d[(c + 1) & 1]);
+    for (int j = 0; j < 16; j += 2) acc[c * 8 + j / 2] = fma2(ff[c / 4], pack2(d[c & 1][j], d[c & 1][j + 1]), acc[c * 8 + j / 2]);
+    if (c + 1 < 8) tmem_ld_wait(d[(c + 1) & 1]);
   }
 }
 
@@ -79,26 +82,27 @@ __device__ __forceinline__ void store_out4(const Out& o, int64_t m, int64_t n, f
   if (n + 2 < o.N) p[2] = v.z;
 }
 
-// A warp's 32 rows x COLS columns (row m0 + lane in this lane's registers) to memory, 32 columns at a time through 4 KB of shared
-// memory: lanes write their own rows and read four rows of 128 bytes, so that every store instruction fills whole lines (fp32; half
-// lines in bf16).  Pieces of 16 bytes lie at piece ^ (row % 8): no bank conflicts either way.
-template <int COLS>
-__device__ __forceinline__ void store_tile(const Out& o, unsigned char* stage, const uint64_t (&acc)[COLS / 2], int64_t m0, int64_t n0, int lane) {
+// A warp's 32 rows (row m0 + lane in this lane's registers) of the runs at columns n0 and n1 to memory, 16 columns at a time through
+// 2 KB of shared memory: lanes write their own rows and read eight rows of 64 bytes, so that a store instruction fills whole sectors.
+// Pieces of 16 bytes lie at piece ^ (row / 2 % 4): no bank conflicts either way.
+constexpr int kStoreBytes = 2048;
+__device__ __forceinline__ unsigned char* store_piece(unsigned char* stage, int row, int piece) { return stage + row * 64 + ((piece ^ (row >> 1 & 3)) << 4); }
+__device__ __forceinline__ void store_tile(const Out& o, unsigned char* stage, const uint64_t (&acc)[kRun], int64_t m0, int64_t n0, int64_t n1, int lane) {
 #pragma unroll
-  for (int c = 0; c < COLS / 32; c++) {
+  for (int c = 0; c < 8; c++) {
     __syncwarp();                                       // the chunk before has been read
 #pragma unroll
-    for (int p = 0; p < 8; p++) {
+    for (int p = 0; p < 4; p++) {
       float v[4];
-      unpack2(acc[c * 16 + 2 * p], v[0], v[1]);
-      unpack2(acc[c * 16 + 2 * p + 1], v[2], v[3]);
-      *reinterpret_cast<float4*>(swz(stage, lane, p)) = make_float4(v[0], v[1], v[2], v[3]);
+      unpack2(acc[c * 8 + 2 * p], v[0], v[1]);
+      unpack2(acc[c * 8 + 2 * p + 1], v[2], v[3]);
+      *reinterpret_cast<float4*>(store_piece(stage, lane, p)) = make_float4(v[0], v[1], v[2], v[3]);
     }
     __syncwarp();
 #pragma unroll
-    for (int i = 0; i < 8; i++) {
-      const int row = i * 4 + lane / 8, piece = lane % 8;
-      store_out4(o, m0 + row, n0 + c * 32 + piece * 4, *reinterpret_cast<const float4*>(swz(stage, row, piece)));
+    for (int i = 0; i < 4; i++) {
+      const int row = i * 8 + lane / 4, piece = lane % 4;
+      store_out4(o, m0 + row, (c < 4 ? n0 : n1) + (c % 4) * 16 + piece * 4, *reinterpret_cast<const float4*>(store_piece(stage, row, piece)));
     }
   }
 }
@@ -108,14 +112,15 @@ __device__ __forceinline__ void store_tile(const Out& o, unsigned char* stage, c
 template <int TN>
 __device__ __forceinline__ int part_offset(int row, int u) { return row * (TN * 4) + ((u ^ (row & 7)) << 4); }
 
-template <int TN, int COLS>
-__device__ __forceinline__ void stage_part(unsigned char* base, const uint64_t (&acc)[COLS / 2], int row, int col0) {
+// A thread's runs at columns c0 and c1 of the tile.
+template <int TN>
+__device__ __forceinline__ void stage_part(unsigned char* base, const uint64_t (&acc)[kRun], int row, int c0, int c1) {
 #pragma unroll
-  for (int p = 0; p < COLS / 4; p++) {
+  for (int p = 0; p < 32; p++) {
     float v[4];
     unpack2(acc[2 * p], v[0], v[1]);
     unpack2(acc[2 * p + 1], v[2], v[3]);
-    *reinterpret_cast<float4*>(base + part_offset<TN>(row, col0 / 4 + p)) = make_float4(v[0], v[1], v[2], v[3]);
+    *reinterpret_cast<float4*>(base + part_offset<TN>(row, (p < 16 ? c0 : c1) / 4 + p % 16)) = make_float4(v[0], v[1], v[2], v[3]);
   }
 }
 __device__ __forceinline__ float4 ld_cluster16(uint32_t addr) {

@@ -172,6 +172,9 @@ __device__ __forceinline__ void tmem_st16(uint32_t addr, const uint32_t (&v)[16]
       ::"r"(addr), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]),
         "r"(v[8]), "r"(v[9]), "r"(v[10]), "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15]) : "memory");
 }
+__device__ __forceinline__ void tmem_st4(uint32_t addr, const uint32_t (&v)[4]) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x4.b32 [%0], {%1,%2,%3,%4};" ::"r"(addr), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]) : "memory");
+}
 __device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 // D[tmem] (+)= A[tmem] * B[smem desc]^T, 128 x N x 16, 16-bit operands (type by the instruction descriptor), fp32
 // accumulate.  A: row r in lane r, the 16 K-elements in 8 consecutive 32-bit columns (two per column, the
@@ -214,6 +217,14 @@ __device__ __forceinline__ void umma_bf16(uint32_t d_tmem, uint64_t a_desc, uint
 __device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, int src_bytes) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;\n" ::"r"(dst), "l"(src), "r"(src_bytes) : "memory");
 }
+__device__ __forceinline__ void cp_async4(uint32_t dst, const void* src, int src_bytes) {
+  asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;\n" ::"r"(dst), "l"(src), "r"(src_bytes) : "memory");
+}
+// This thread arrives on the barrier (one of the arrivals it was initialised for) once its copies so far have landed.
+__device__ __forceinline__ void cp_async_arrive(uint64_t* bar) {
+  asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
+}
+__device__ __forceinline__ void cp_async_wait_all() { asm volatile("cp.async.wait_all;" ::: "memory"); }
 __device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;\n" ::: "memory"); }
 template <int N> __device__ __forceinline__ void cp_async_wait() { asm volatile("cp.async.wait_group %0;\n" ::"n"(N) : "memory"); }
 // D[tmem] = A[smem desc] * B[smem desc]^T, 128 x N x 16, bf16 operands, fp32 result (overwrites).
@@ -245,6 +256,32 @@ __device__ __forceinline__ uint32_t mapa_rank(uint32_t addr, uint32_t rank) {
 __device__ __forceinline__ void mbar_arrive_cluster(uint32_t cluster_addr) {
   asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
 }
+// A word to the shared memory of a CTA of the cluster; its four bytes complete on a barrier of that CTA, so that whoever waits there
+// sees it and the writer waits for nothing (a store and an arrival that releases it take 2600 clk beside a stream of tensor copies).
+__device__ __forceinline__ void st_async_u32(uint32_t cluster_addr, uint32_t v, uint32_t cluster_bar) {
+  asm volatile("st.async.weak.shared::cluster.mbarrier::complete_tx::bytes.u32 [%0], %1, [%2];" ::"r"(cluster_addr), "r"(v), "r"(cluster_bar) : "memory");
+}
+// Bounded waits with the limit in a register: read from memory where a wait blocks, it costs every such wait a load, and a load
+// behind 192 KB of tensor copies takes 2 to 3 us.
+struct Waiter {
+  uint32_t limit;
+  volatile int* abort_flag;
+  __device__ __forceinline__ bool operator()(uint32_t bar, uint32_t parity, int code) const {
+    if (mbar_try_wait_a(bar, parity)) return true;
+    for (uint32_t it = 0; it < limit; it++) {
+      if (mbar_try_wait_a(bar, parity)) return true;
+      if (*abort_flag) return false;
+    }
+    atomicCAS(&g_error_word, 0, code);
+    *abort_flag = 1;
+    return false;
+  }
+};
+// The same for an arrival that only says that this thread has read (tensor memory, shared memory): nothing that it wrote has to be
+// seen by the other CTA.  The release above waits for the thread's stores, 2600 clk behind a tile's.
+__device__ __forceinline__ void mbar_arrive_cluster_read(uint32_t cluster_addr) {
+  asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
+}
 // Tensor memory of both CTAs at once: the same warp of each CTA executes these with the same arguments.
 __device__ __forceinline__ void tmem_alloc_pair(uint32_t* dst_smem, uint32_t cols) {
   asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(dst_smem)), "r"(cols));
@@ -267,6 +304,16 @@ __device__ __forceinline__ void umma_f8_pair(uint32_t d_tmem, uint64_t a_desc, u
       "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
       "tcgen05.mma.cta_group::2.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}"
       ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate) : "memory");
+}
+// The same with a power of two per row of A and per row of B on this step's 32 elements (UE8M0 bytes in tensor memory: row r's in
+// lane r % 32 of every 32 lanes, column r / 32 from the address on; the instruction descriptor says which byte of that word).
+// Each CTA's tensor memory holds the factors of its own 128 rows of A and of all N rows of B.
+__device__ __forceinline__ void umma_mxf8_pair(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t sa_tmem, uint32_t sb_tmem,
+                                               uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %6, 0;\n\t"
+      "tcgen05.mma.cta_group::2.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], %1, %2, %3, [%4], [%5], p;\n\t}"
+      ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(sa_tmem), "r"(sb_tmem), "r"(accumulate) : "memory");
 }
 // Arrives, once the pair's MMAs issued so far have completed, on the barrier at this address in every CTA of the mask.
 __device__ __forceinline__ void umma_commit_pair_mc(uint32_t bar, uint16_t cta_mask) {
@@ -318,6 +365,11 @@ __host__ __device__ constexpr uint32_t instr_desc_pair(int n, uint32_t ab_format
   return (1u << 4) | (ab_format << 7) | (ab_format << 10) | (static_cast<uint32_t>(n >> 3) << 17) |
          (static_cast<uint32_t>((2 * TM) >> 4) << 24);
 }
+// The same for block-scaled e4m3 operands with UE8M0 factors; byte: which one of the word that holds a row's factors (both operands).
+__host__ __device__ constexpr uint32_t instr_desc_mx_pair(int n) {
+  return (static_cast<uint32_t>(n >> 3) << 17) | (1u << 23) | (static_cast<uint32_t>((2 * TM) >> 7) << 27);
+}
+__host__ __device__ constexpr uint32_t instr_desc_mx_byte(uint32_t byte) { return (byte << 4) | (byte << 29); }
 // Added to an instruction descriptor: that operand is MN-major (its contraction index is the outer one in memory).
 constexpr uint32_t kTransposeA = 1u << 15, kTransposeB = 1u << 16;
 constexpr uint32_t kFmtE4M3 = 0, kFmtBF16 = 1;   // kind::f8f6f4 / kind::f16 operand codes

@@ -147,6 +147,61 @@ def test_weight_grad_rounds_other_scales_to_bf16(hb):
     assert (np.abs(GW.double().cpu().numpy() - g.T @ x) <= bound).all()
 
 
+def on_device(held):
+    """An operand's values in 64 bits on the device, from its codes and scales by torch's own conversions."""
+    op = held[0]
+    return op.codes.view(torch.float8_e4m3fn)[:, :op.K].double() * op.scales.double().repeat_interleave(op.block_rows, 0)[:op.rows].repeat_interleave(128, 1)[:, :op.K]
+
+
+@pytest.mark.parametrize("kind", ["gemm", "input_grad"])
+@pytest.mark.parametrize("M,N,K,scales", [(2600, 2300, 640, "pow2"), (5000, 2050, 130, "pow2"), (2600, 2300, 640, "any"), (2600, 2300, 640, "mixed"),
+                                          (1300, 4100, 2500, "mixed"), (2100, 2100, 1100, "pow2")])
+def test_products_of_many_tiles(hb, M, N, K, scales, kind):
+    """More tiles than the machine holds at once, every row, column block and group of its own magnitude: a scale, a partial sum or
+    a staged row of another tile shows.  mixed: some groups' scales are powers of two and some are not."""
+    rng = np.random.default_rng(M + N)
+    n_a, rows_w, cols_w = (K, N, K) if kind == "gemm" else (N, N, K)
+
+    def spreads(rows, cols, per_row, per_col):
+        e = rng.integers(-12, 12, (-(-rows // per_row), 1)).repeat(per_row, 0)[:rows] + rng.integers(-6, 6, (1, -(-cols // per_col))).repeat(per_col, 1)[:, :cols]
+        return np.exp2(e).astype(np.float32)
+    A = fu.held(normal(M, n_a, M + 1, False) * spreads(M, n_a, 1, 128), 1)
+    W = fu.held(normal(rows_w, cols_w, N + 2, False) * spreads(rows_w, cols_w, 128, 128), 128)
+    for op, br in ((A[0], 1), (W[0], 128)):
+        s = op.scales
+        if scales != "pow2":
+            f = torch.from_numpy(rng.uniform(1.0, 1.99, tuple(s.shape)).astype(np.float32)).cuda()
+            if scales == "mixed":                              # whole runs of groups, and single entries of others
+                keep = torch.from_numpy(rng.random((1, s.shape[1])) < 0.6).cuda() | (torch.from_numpy(rng.random(tuple(s.shape)) < 0.998).cuda())
+                f = torch.where(keep, 1.0, f)
+            s.mul_(f)
+    a, w = on_device(A), on_device(W)
+    out, clean = fu.framed(M, N if kind == "gemm" else K, torch.float32, 8)
+    (hb.fp8_gemm if kind == "gemm" else hb.fp8_input_grad)(A[0], W[0], out)
+    w = w.t() if kind == "gemm" else w
+    ref, F = a @ w, a.abs() @ w.abs()
+    assert ((out.double() - ref).abs() <= product_bound(F, ref, -(-n_a // 128), "fp32")).all()
+    assert clean()
+
+
+@pytest.mark.parametrize("M,N,K,scales", [(256, 256, 640, "any"), (200, 500, 1500, "any"), (300, 1000, 4096, "any"), (300, 1000, 4096, "pow2"),
+                                          (20, 136, 9216, "any"), (700, 700, 10000, "pow2")])
+def test_products_of_few_tiles_again_and_again(hb, M, N, K, scales):
+    """Tiles that several pairs share (and one accumulator after another along a long K): the same bits every time, whatever ran
+    before."""
+    A, a, _, _ = fu.held(normal(M, K, M + K), 1, scales)
+    W, w, _, _ = fu.held(normal(N, K, N + K, False), 128, scales)
+    first = hb.fp8_gemm(A, W, torch.empty(M, -(-N // 4) * 4, device="cuda")[:, :N])
+    ref, F = a @ w.T, np.abs(a) @ np.abs(w).T
+    assert (np.abs(first.double().cpu().numpy() - ref) <= product_bound(F, ref, -(-K // 128), "fp32")).all()
+    spoil = torch.empty(1 << 26, device="cuda")
+    for i in range(30):
+        if i % 3 == 0:
+            spoil.fill_(float("nan"))
+        C = torch.full((M, -(-N // 4) * 4), float("nan"), device="cuda")[:, :N]
+        assert torch.equal(hb.fp8_gemm(A, W, C), first), i
+
+
 def test_a_nan_stays_in_its_row_and_column(hb):
     a, w = normal(150, 300, 11), normal(260, 300, 12, False)
     a[77, 200], w[130, 299] = np.nan, np.inf
