@@ -480,7 +480,7 @@ hbmm_status hbmm_fp8_binarize_backward(const hbmm_fp8_operand *X, const void *gy
  * 8 the warps that compute them, 9 the self-test of hbmm_debug_expire_wait; reported as they are for
  * the e4m3 HBMM kernel, 100 + code for the HBWN kernel, 200 + code for the packed convolution front end
  * (201 loader, 202-204 compute warps), 300 + code for the folded-scale HBMM kernel, 400 + code for the
- * products of 8-bit operands.
+ * products of 8-bit operands, 500 + code for the weight gradient from one.
  * Lifetime: one word per kernel family and process, holding the FIRST code recorded since it was last
  * cleared; nothing but hbmm_clear_device_error resets it, so after one expiry every later query reports
  * HBMM_ERR_TIMEOUT, whichever call it follows, until the word is cleared.

@@ -543,6 +543,9 @@ hbmm_status hbmm_last_device_error(int32_t* code) {
   int c5 = 0;
   if (fp8_gemm_health(kHealthRead, &c5) != cudaSuccess) return HBMM_ERR_CUDA;
   if (c == 0 && c5 != 0) c = 400 + c5;    // the products of 8-bit operands
+  int c6 = 0;
+  if (fp8_weight_grad_health(kHealthRead, &c6) != cudaSuccess) return HBMM_ERR_CUDA;
+  if (c == 0 && c6 != 0) c = 500 + c6;    // the weight gradient from an 8-bit operand
   if (code) *code = c;
   return c == 0 ? HBMM_OK : HBMM_ERR_TIMEOUT;
 }
@@ -551,7 +554,7 @@ hbmm_status hbmm_clear_device_error(void) {
   int unused = 0;
   if (gemm_umma_health(kHealthClear, &unused) != cudaSuccess || hbwn_umma_health(kHealthClear, &unused) != cudaSuccess ||
       im2col_tma_health(kHealthClear, &unused) != cudaSuccess || gemm_fold_health(kHealthClear, &unused) != cudaSuccess ||
-      fp8_gemm_health(kHealthClear, &unused) != cudaSuccess)
+      fp8_gemm_health(kHealthClear, &unused) != cudaSuccess || fp8_weight_grad_health(kHealthClear, &unused) != cudaSuccess)
     return HBMM_ERR_CUDA;
   return HBMM_OK;
 }
@@ -561,7 +564,7 @@ hbmm_status hbmm_debug_set_wait_limit(uint32_t polls) {
   if (polls > 0x7FFFFFFFu) return HBMM_ERR_INVALID_ARG;
   if (gemm_umma_health(kHealthSetSpinLimit, &v) != cudaSuccess || hbwn_umma_health(kHealthSetSpinLimit, &v) != cudaSuccess ||
       im2col_tma_health(kHealthSetSpinLimit, &v) != cudaSuccess || gemm_fold_health(kHealthSetSpinLimit, &v) != cudaSuccess ||
-      fp8_gemm_health(kHealthSetSpinLimit, &v) != cudaSuccess)
+      fp8_gemm_health(kHealthSetSpinLimit, &v) != cudaSuccess || fp8_weight_grad_health(kHealthSetSpinLimit, &v) != cudaSuccess)
     return HBMM_ERR_CUDA;
   return HBMM_OK;
 }

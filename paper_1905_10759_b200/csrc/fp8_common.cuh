@@ -49,6 +49,12 @@ __device__ __forceinline__ float2 from_e4m3x2(uint32_t codes) {
   return f;
 }
 
+__device__ __forceinline__ uint32_t bf16x2(float lo, float hi) {
+  uint32_t r;
+  asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+  return r;
+}
+
 // The scale of a group from the bits of its largest finite magnitude: the smallest power of two s with amax / s <= 448, at
 // least 2^-117 (448 = 1.75 * 2^8).  Exponent fields only, so exact for subnormal amax too (their field is 0: the floor).
 __device__ __forceinline__ uint32_t scale_exponent(uint32_t amax_bits) {

@@ -82,28 +82,32 @@ __device__ __forceinline__ void store_out4(const Out& o, int64_t m, int64_t n, f
   if (n + 2 < o.N) p[2] = v.z;
 }
 
-// A warp's 32 rows (row m0 + lane in this lane's registers) of the runs at columns n0 and n1 to memory, 16 columns at a time through
-// 2 KB of shared memory: lanes write their own rows and read eight rows of 64 bytes, so that a store instruction fills whole sectors.
+// A warp's 32 rows (row m0 + lane in this lane's registers) to memory, 16 columns at a time (store_tile: of the runs at columns n0
+// and n1) through 2 KB of shared memory: lanes write their own rows and read eight rows of 64 bytes, so that a store instruction fills whole sectors.
 // Pieces of 16 bytes lie at piece ^ (row / 2 % 4): no bank conflicts either way.
 constexpr int kStoreBytes = 2048;
 __device__ __forceinline__ unsigned char* store_piece(unsigned char* stage, int row, int piece) { return stage + row * 64 + ((piece ^ (row >> 1 & 3)) << 4); }
+__device__ __forceinline__ void store_columns(const Out& o, unsigned char* stage, const uint32_t (&v)[16], int64_t m0, int64_t n0, int lane) {
+  __syncwarp();                                         // the columns before have been read
+#pragma unroll
+  for (int p = 0; p < 4; p++) *reinterpret_cast<uint4*>(store_piece(stage, lane, p)) = make_uint4(v[4 * p], v[4 * p + 1], v[4 * p + 2], v[4 * p + 3]);
+  __syncwarp();
+#pragma unroll
+  for (int i = 0; i < 4; i++) {
+    const int row = i * 8 + lane / 4, piece = lane % 4;
+    store_out4(o, m0 + row, n0 + piece * 4, *reinterpret_cast<const float4*>(store_piece(stage, row, piece)));
+  }
+}
 __device__ __forceinline__ void store_tile(const Out& o, unsigned char* stage, const uint64_t (&acc)[kRun], int64_t m0, int64_t n0, int64_t n1, int lane) {
 #pragma unroll
   for (int c = 0; c < 8; c++) {
-    __syncwarp();                                       // the chunk before has been read
+    uint32_t v[16];
 #pragma unroll
-    for (int p = 0; p < 4; p++) {
-      float v[4];
-      unpack2(acc[c * 8 + 2 * p], v[0], v[1]);
-      unpack2(acc[c * 8 + 2 * p + 1], v[2], v[3]);
-      *reinterpret_cast<float4*>(store_piece(stage, lane, p)) = make_float4(v[0], v[1], v[2], v[3]);
+    for (int p = 0; p < 8; p++) {
+      v[2 * p] = static_cast<uint32_t>(acc[c * 8 + p]);
+      v[2 * p + 1] = static_cast<uint32_t>(acc[c * 8 + p] >> 32);
     }
-    __syncwarp();
-#pragma unroll
-    for (int i = 0; i < 4; i++) {
-      const int row = i * 8 + lane / 4, piece = lane % 4;
-      store_out4(o, m0 + row, (c < 4 ? n0 : n1) + (c % 4) * 16 + piece * 4, *reinterpret_cast<const float4*>(store_piece(stage, row, piece)));
-    }
+    store_columns(o, stage, v, m0, (c < 4 ? n0 : n1) + (c % 4) * 16, lane);
   }
 }
 

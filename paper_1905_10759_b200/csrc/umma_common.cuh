@@ -205,6 +205,11 @@ __device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
   asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
   return r;
 }
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
 // D[tmem] (+)= A[smem desc] * B[smem desc]^T, 128 x N x 16, bf16 (or, by the instruction descriptor, fp16)
 // operands, fp32 accumulate.
 __device__ __forceinline__ void umma_bf16(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
@@ -354,6 +359,11 @@ __device__ __forceinline__ uint64_t smem_desc(uint32_t addr) {
   d |= static_cast<uint64_t>(1) << 46;
   d |= static_cast<uint64_t>(2) << 61;
   return d;
+}
+// The same for an MN-major operand: rows of the contraction of 128 bytes, 8-row groups 1024 bytes apart; every 128 bytes of columns are
+// a tile of their own, `tile_bytes` after the one before.
+__device__ __forceinline__ uint64_t smem_desc_mn(uint32_t addr, uint32_t tile_bytes) {
+  return (smem_desc(addr) & ~(static_cast<uint64_t>(0x3FFF) << 16)) | static_cast<uint64_t>(tile_bytes >> 4) << 16;
 }
 // Instruction descriptors: fp32 accumulator, both operands K-major, M = 128, N = n.
 __host__ __device__ constexpr uint32_t instr_desc(int n, uint32_t ab_format) {

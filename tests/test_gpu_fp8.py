@@ -134,6 +134,32 @@ def test_weight_grad(hb, M, N, K, base):
         assert torch.equal(b, b0)
 
 
+@pytest.mark.parametrize("M,N,K,base", [(300, 2600, 2300, True), (8300, 2304, 2310, False), (16500, 2200, 2600, True)])
+def test_weight_grad_of_many_tiles(hb, M, N, K, base):
+    """More tiles than the machine holds at once, rows and groups of their own magnitude, and more rows than one accumulator takes."""
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(M)
+    x = torch.randn(M, K, generator=gen, device="cuda") * torch.exp2(torch.randint(-8, 8, (M, 1), generator=gen, device="cuda").float())
+    x *= torch.exp2(torch.randint(-6, 6, (1, -(-K // 128)), generator=gen, device="cuda").float()).repeat_interleave(128, 1)[:, :K]
+    gy = (torch.randn(M, N, generator=gen, device="cuda") * torch.exp2(torch.randint(-8, 8, (1, N), generator=gen, device="cuda").float())).bfloat16()
+    X = hb.fp8_quantize(x, hb.alloc_fp8_operand(M, K))
+    xv, g = on_device((X,)), gy.double()
+    GW, clean = fu.framed(N, K, torch.float32, 4)
+    b = torch.randn(N, -(-K // 4) * 4, generator=gen, device="cuda")[:, :K] if base else None
+    hb.fp8_weight_grad(gy, X, GW, base=b)
+    ref = g.t() @ xv
+    bound = (2 * M + 2) * fu.U * (g.abs().t() @ xv.abs())
+    if base:
+        ref += b.double()
+    bound += 2 * fu.U * ref.abs() * (M // 8192 + 1)
+    assert ((GW.double() - ref).abs() <= bound).all()
+    # far inside that bound where nothing cancels: the sums' errors do not pile up row by row
+    assert (GW.double() - ref).norm() <= 4e-6 * ref.norm()
+    assert clean()
+    again = torch.full((N, -(-K // 4) * 4), float("nan"), device="cuda")[:, :K]
+    assert torch.equal(hb.fp8_weight_grad(gy, X, again, base=b), GW)
+
+
 def test_weight_grad_rounds_other_scales_to_bf16(hb):
     """Scales that are no powers of two: X^ is the bf16 number next to code times scale."""
     X, x, _, _ = fu.held(normal(200, 300, 5), 1, "any")
