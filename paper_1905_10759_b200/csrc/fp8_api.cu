@@ -70,6 +70,8 @@ hbmm_status hbmm_fp8_gemm(const hbmm_fp8_operand* A, const hbmm_fp8_operand* W, 
   if (st != HBMM_OK) return st;
   if (A->K != W->K || !valid_dtype(c_dtype)) return HBMM_ERR_INVALID_ARG;
   if ((st = check_rows(C, W->rows, ldc, size_of(c_dtype))) != HBMM_OK) return st;
+  if (fp8_gemv_supported(view_of(A)))
+    return status_of(launch_fp8_gemv(view_of(A), view_of(W), C, c_dtype == HBMM_BF16, ldc, static_cast<cudaStream_t>(stream)));
   return status_of(launch_fp8_gemm(view_of(A), view_of(W), false, C, c_dtype == HBMM_BF16, ldc, static_cast<cudaStream_t>(stream)));
 }
 

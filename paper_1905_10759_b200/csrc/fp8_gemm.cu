@@ -425,7 +425,7 @@ fp8_gemm_kernel(const Args g, const __grid_constant__ CUtensorMap a_map, const _
       }
       if (ok && open != 0 && !take_accumulator()) ok = false;
       if (!ok) break;
-      if (g.parts == 1) store_tile(g.out, stage, acc, m0 + (warp & 3) * 32, n0 + 64 * h, n0 + 128 + 64 * h, lane);
+      if (g.parts == 1) store_tile<false>(g.out, stage, acc, m0 + (warp & 3) * 32, n0 + 64 * h, n0 + 128 + 64 * h, lane);
     }
     if (g.parts > 1) {
       // The partial sums of this CTA's only tile take the stages' place, once both warpgroups have seen their last unit: the MMAs

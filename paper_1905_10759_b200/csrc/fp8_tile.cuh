@@ -54,8 +54,7 @@ __device__ __forceinline__ void store_out4(const Out& o, int64_t m, int64_t n, f
   if (o.bf16) {
     __nv_bfloat16* p = static_cast<__nv_bfloat16*>(o.c) + m * o.ldc + n;
     if (whole) {
-      const __nv_bfloat162 a = __floats2bfloat162_rn(v.x, v.y), b = __floats2bfloat162_rn(v.z, v.w);
-      *reinterpret_cast<uint2*>(p) = make_uint2(*reinterpret_cast<const uint32_t*>(&a), *reinterpret_cast<const uint32_t*>(&b));
+      *reinterpret_cast<uint2*>(p) = make_uint2(bf16x2(v.x, v.y), bf16x2(v.z, v.w));
       return;
     }
     const float e[4] = {v.x, v.y, v.z, v.w};
@@ -82,32 +81,88 @@ __device__ __forceinline__ void store_out4(const Out& o, int64_t m, int64_t n, f
   if (n + 2 < o.N) p[2] = v.z;
 }
 
-// A warp's 32 rows (row m0 + lane in this lane's registers) to memory, 16 columns at a time (store_tile: of the runs at columns n0
-// and n1) through 2 KB of shared memory: lanes write their own rows and read eight rows of 64 bytes, so that a store instruction fills whole sectors.
-// Pieces of 16 bytes lie at piece ^ (row / 2 % 4): no bank conflicts either way.
+// A warp's 32 rows (row m0 + lane in this lane's registers) of the runs at columns n0 and n1 to memory, 16 columns at a time through
+// 2 KB of shared memory: lanes write their own rows and read eight rows of 64 bytes (32 columns in bf16), so that a store instruction fills whole sectors.
+// Pieces of 16 bytes lie at piece ^ (row / 2 % 4): no bank conflicts either way.  A block that lies inside the matrix goes without
+// checks, its base (if any) 16 columns ahead of its use: 32 loads one after another took 26 us per tile.
 constexpr int kStoreBytes = 2048;
 __device__ __forceinline__ unsigned char* store_piece(unsigned char* stage, int row, int piece) { return stage + row * 64 + ((piece ^ (row >> 1 & 3)) << 4); }
-__device__ __forceinline__ void store_columns(const Out& o, unsigned char* stage, const uint32_t (&v)[16], int64_t m0, int64_t n0, int lane) {
-  __syncwarp();                                         // the columns before have been read
+// The base's lines of a warp's 32 rows x 128 columns into L2, some time before store_tile reads them.
+__device__ __forceinline__ void prefetch_base(const Out& o, int64_t m0, int64_t n0, int lane) {
+  if (!o.base || m0 + lane >= o.M) return;
 #pragma unroll
-  for (int p = 0; p < 4; p++) *reinterpret_cast<uint4*>(store_piece(stage, lane, p)) = make_uint4(v[4 * p], v[4 * p + 1], v[4 * p + 2], v[4 * p + 3]);
-  __syncwarp();
-#pragma unroll
-  for (int i = 0; i < 4; i++) {
-    const int row = i * 8 + lane / 4, piece = lane % 4;
-    store_out4(o, m0 + row, n0 + piece * 4, *reinterpret_cast<const float4*>(store_piece(stage, row, piece)));
-  }
+  for (int c = 0; c < 4; c++)
+    if (n0 + c * 32 < o.N) asm volatile("prefetch.global.L2 [%0];" ::"l"(o.base + (m0 + lane) * o.ld_base + n0 + c * 32));
 }
+template <bool BASE>
 __device__ __forceinline__ void store_tile(const Out& o, unsigned char* stage, const uint64_t (&acc)[kRun], int64_t m0, int64_t n0, int64_t n1, int lane) {
+  const int sub = lane / 4, piece = lane % 4;
+  const int64_t r0 = m0 + sub;
+  const bool inside = m0 + 32 <= o.M && n0 + kRun <= o.N && n1 + kRun <= o.N;
+  if (!BASE && inside && o.bf16) {                      // 32 columns at a time, rounded on the way in
+    __nv_bfloat16* out = static_cast<__nv_bfloat16*>(o.c) + r0 * o.ldc + n0 + piece * 8;
+#pragma unroll
+    for (int c = 0; c < 4; c++) {
+      __syncwarp();
+#pragma unroll
+      for (int p = 0; p < 4; p++) {
+        uint32_t w[4];
+#pragma unroll
+        for (int e = 0; e < 4; e++) {
+          float lo, hi;
+          unpack2(acc[c * 16 + p * 4 + e], lo, hi);
+          w[e] = bf16x2(lo, hi);
+        }
+        *reinterpret_cast<uint4*>(store_piece(stage, lane, p)) = make_uint4(w[0], w[1], w[2], w[3]);
+      }
+      __syncwarp();
+#pragma unroll
+      for (int i = 0; i < 4; i++)
+        *reinterpret_cast<uint4*>(out + i * 8 * o.ldc) = *reinterpret_cast<const uint4*>(store_piece(stage, i * 8 + sub, piece));
+      out += c == 1 ? n1 - n0 - 32 : 32;
+    }
+    return;
+  }
+  const bool plain = inside && !o.bf16;
+  float* out = static_cast<float*>(o.c) + r0 * o.ldc + n0 + piece * 4;
+  const bool base = BASE && plain && o.base != nullptr;
+  const float* from = base ? o.base + r0 * o.ld_base + n0 + piece * 4 : nullptr;
+  uint4 ahead[4];
+  if (BASE && base) {
+#pragma unroll
+    for (int i = 0; i < 4; i++) ahead[i] = load16(from + i * 8 * o.ld_base);
+  }
 #pragma unroll
   for (int c = 0; c < 8; c++) {
-    uint32_t v[16];
+    __syncwarp();                                       // the columns before have been read
 #pragma unroll
-    for (int p = 0; p < 8; p++) {
-      v[2 * p] = static_cast<uint32_t>(acc[c * 8 + p]);
-      v[2 * p + 1] = static_cast<uint32_t>(acc[c * 8 + p] >> 32);
+    for (int p = 0; p < 4; p++)
+      *reinterpret_cast<uint4*>(store_piece(stage, lane, p)) =
+          make_uint4(static_cast<uint32_t>(acc[c * 8 + 2 * p]), static_cast<uint32_t>(acc[c * 8 + 2 * p] >> 32),
+                     static_cast<uint32_t>(acc[c * 8 + 2 * p + 1]), static_cast<uint32_t>(acc[c * 8 + 2 * p + 1] >> 32));
+    __syncwarp();
+    if (plain) {
+#pragma unroll
+      for (int i = 0; i < 4; i++) {
+        float4 v = *reinterpret_cast<const float4*>(store_piece(stage, i * 8 + sub, piece));
+        if (BASE && base) {
+          v.x += __uint_as_float(ahead[i].x); v.y += __uint_as_float(ahead[i].y);
+          v.z += __uint_as_float(ahead[i].z); v.w += __uint_as_float(ahead[i].w);
+        }
+        *reinterpret_cast<float4*>(out + i * 8 * o.ldc) = v;
+      }
+      const int64_t on = c == 3 ? n1 - n0 - kRun + 16 : 16;
+      out += on;
+      if (BASE && base && c < 7) {
+        from += on;
+#pragma unroll
+        for (int i = 0; i < 4; i++) ahead[i] = load16(from + i * 8 * o.ld_base);
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; i++)
+        store_out4(o, r0 + i * 8, (c < 4 ? n0 : n1) + (c % 4) * 16 + piece * 4, *reinterpret_cast<const float4*>(store_piece(stage, i * 8 + sub, piece)));
     }
-    store_columns(o, stage, v, m0, (c < 4 ? n0 : n1) + (c % 4) * 16, lane);
   }
 }
 

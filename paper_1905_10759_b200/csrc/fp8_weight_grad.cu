@@ -38,7 +38,7 @@ constexpr int kMostParts = 4;
 // An accumulator in tensor memory takes 512 rows, the epilogue adds it to fp32 registers: the tensor cores' additions truncate, always
 // towards zero, and with 8192 rows of sizes from 2^-8 to 2^8 in one accumulator the result was 9e-6 off.
 constexpr int kChunkStages = 512 / ROWS;
-constexpr int kRegsEpilogue = 168, kRegsOthers = 48;         // 256 x 168 + 384 x 48 = the 640 x 96 registers at launch
+constexpr int kRegsEpilogue = 176, kRegsOthers = 40;         // 256 x 176 + 384 x 40 of the 640 x 96 registers at launch
 static_assert(kBytes <= 227 * 1024 && TM * TN * 4 <= OFF_CODES, "shared memory");
 
 struct Args {
@@ -75,10 +75,10 @@ fp8_weight_grad_kernel(const Args g, const __grid_constant__ CUtensorMap gy_map,
     for (int s = 0; s < STAGES; s++) {
       mbar_init(&afull[s], 1);
       mbar_init(&cfull[s], 1);
-      mbar_init(&bfull[s], 2 * kConvertWarps);
+      mbar_init(&bfull[s], kConvertWarps);                  // one half of the converters of each CTA
       mbar_init(&empty[s], 1);
     }
-    for (int s = 0; s < kSlots; s++) { mbar_init(&sfull[s], 32); mbar_init(&sempty[s], kConvertWarps); }
+    for (int s = 0; s < kSlots; s++) { mbar_init(&sfull[s], 32); mbar_init(&sempty[s], kConvertWarps / 2); }
     for (int b = 0; b < 2; b++) { mbar_init(&tfull[b], 1); mbar_init(&tempty[b], 2 * kEpilogueWarps); }
     mbar_init(drained, 1);
     *abort_flag = 0;
@@ -161,43 +161,46 @@ fp8_weight_grad_kernel(const Args g, const __grid_constant__ CUtensorMap gy_map,
     __syncwarp();
   } else if (warp >= kConvertWarp) {
     // =========================== converters (both CTAs) ===========================
-    const int me = tid - kConvertWarp * 32;
+    // Four warps per stage, the other four on the next one: a warp's waits and its fence come once per four items of work.
+    const int me = tid - kConvertWarp * 32 & 127;
+    const uint32_t mine = (warp - kConvertWarp) / 4;
     const uint32_t bfull0 = mapa_rank(smem_u32(bfull), lead);
-    uint32_t s = 0, par = 0, f = 0, f_par = 0;
+    const int q = me & 7;                                // 16 codes from column 16 q, rows me / 8 + 16 i
+    uint32_t s = 0, par = 0, f = 0, f_par = 0, turn = 0;
     bool ok = true;
     for (int64_t tile = walker; tile < n_tiles && ok; tile += walkers) {
-      for (int st = s0; st < s1; st++) {
-        if (!wait(smem_u32(&sfull[f]), f_par, 7) || !wait(smem_u32(&cfull[s]), par, 7)) { ok = false; break; }
-        const float* scales = reinterpret_cast<const float*>(smem + OFF_SCALES + f * ROWS * 4);
-        const unsigned char* codes = smem + OFF_CODES + s * kCodes;
-        unsigned char* b = smem + OFF_B + s * kOperand;
-#pragma unroll
-        for (int i = 0; i < ROWS * 8 / (kConvertWarps * 32); i++) {
-          const int item = i * kConvertWarps * 32 + me, m = item >> 3, q = item & 7;       // 16 codes from column 16 q of row m
-          const uint4 c = *reinterpret_cast<const uint4*>(codes + m * 128 + q * 16);
-          const float sc = scales[m];
-          const uint32_t w[4] = {c.x, c.y, c.z, c.w};
-          uint32_t o[8];
-#pragma unroll
-          for (int e = 0; e < 4; e++) {
-            const float2 lo = from_e4m3x2(w[e] & 0xFFFFu), hi = from_e4m3x2(w[e] >> 16);
-            o[2 * e] = bf16x2(lo.x * sc, lo.y * sc);
-            o[2 * e + 1] = bf16x2(hi.x * sc, hi.y * sc);
-          }
+      for (int st = s0; st < s1; st++, turn ^= 1) {
+        if (turn == mine) {
+          if (!wait(smem_u32(&sfull[f]), f_par, 7) || !wait(smem_u32(&cfull[s]), par, 7)) { ok = false; break; }
+          const float* scales = reinterpret_cast<const float*>(smem + OFF_SCALES + f * ROWS * 4) + (me >> 3);
+          const unsigned char* codes = smem + OFF_CODES + s * kCodes + me * 16;
           // two 16-byte pieces of the row's 64 columns; lanes of the second 64 columns store theirs in the other order, so that the
-          // eight lanes of a row hit different banks
-          unsigned char* rows64 = b + (q >> 2) * kChunkBytes;
-          const uint4 p0 = make_uint4(o[0], o[1], o[2], o[3]), p1 = make_uint4(o[4], o[5], o[6], o[7]);
+          // eight lanes of a row hit different banks (rows 16 apart share their swizzle)
           const bool swap = (q & 4) != 0;
-          const int first = 2 * (q & 3) + (swap ? 1 : 0);
-          *reinterpret_cast<uint4*>(swz(rows64, m, first)) = swap ? p1 : p0;
-          *reinterpret_cast<uint4*>(swz(rows64, m, first ^ 1)) = swap ? p0 : p1;
-        }
-        fence_async_proxy();                             // the stores are the tensor core's to read
-        __syncwarp();
-        if (lane == 0) {
-          mbar_arrive_cluster_read(bfull0 + s * 8);
-          mbar_arrive(&sempty[f]);
+          unsigned char* rows64 = smem + OFF_B + s * kOperand + (q >> 2) * kChunkBytes;
+          unsigned char* to0 = swz(rows64, me >> 3, 2 * (q & 3) + (swap ? 1 : 0));
+          unsigned char* to1 = swz(rows64, me >> 3, 2 * (q & 3) + (swap ? 0 : 1));
+#pragma unroll
+          for (int i = 0; i < ROWS / 16; i++) {
+            const uint4 c = *reinterpret_cast<const uint4*>(codes + i * 16 * 128);
+            const float sc = scales[i * 16];
+            const uint32_t w[4] = {c.x, c.y, c.z, c.w};
+            uint32_t o[8];
+#pragma unroll
+            for (int e = 0; e < 4; e++) {
+              const float2 lo = from_e4m3x2(w[e] & 0xFFFFu), hi = from_e4m3x2(w[e] >> 16);
+              o[2 * e] = bf16x2(lo.x * sc, lo.y * sc);
+              o[2 * e + 1] = bf16x2(hi.x * sc, hi.y * sc);
+            }
+            *reinterpret_cast<uint4*>(to0 + i * 16 * 128) = swap ? make_uint4(o[4], o[5], o[6], o[7]) : make_uint4(o[0], o[1], o[2], o[3]);
+            *reinterpret_cast<uint4*>(to1 + i * 16 * 128) = swap ? make_uint4(o[0], o[1], o[2], o[3]) : make_uint4(o[4], o[5], o[6], o[7]);
+          }
+          fence_async_proxy();                           // the stores are the tensor core's to read
+          __syncwarp();
+          if (lane == 0) {
+            mbar_arrive_cluster_read(bfull0 + s * 8);
+            mbar_arrive(&sempty[f]);
+          }
         }
         if (++s == STAGES) { s = 0; par ^= 1; }
         if (++f == kSlots) { f = 0; f_par ^= 1; }
@@ -254,6 +257,10 @@ fp8_weight_grad_kernel(const Args g, const __grid_constant__ CUtensorMap gy_map,
       uint64_t acc[kRun];
 #pragma unroll
       for (int j = 0; j < kRun; j++) acc[j] = 0ull;
+      int64_t tm, tn;
+      tile_at(tile, tiles_m, tiles_n, &tm, &tn);
+      const int64_t m0 = tm * 2 * TM + half * TM + (warp & 3) * 32, n0 = tn * TN + col0;
+      if (g.parts == 1) prefetch_base(g.out, m0, n0, lane);
       for (int c0 = s0; c0 < s1; c0 += kChunkStages, n++) {
         const uint32_t buf = n & 1;
         if (!wait(smem_u32(&tfull[buf]), (n >> 1) & 1, 5)) { ok = false; break; }
@@ -271,9 +278,7 @@ fp8_weight_grad_kernel(const Args g, const __grid_constant__ CUtensorMap gy_map,
         if (lane == 0) mbar_arrive_cluster_read(tempty0 + buf * 8);
       }
       if (!ok) break;
-      int64_t tm, tn;
-      tile_at(tile, tiles_m, tiles_n, &tm, &tn);
-      if (g.parts == 1) store_tile(g.out, stage, acc, tm * 2 * TM + half * TM + (warp & 3) * 32, tn * TN + col0, tn * TN + col0 + kRun, lane);
+      if (g.parts == 1) store_tile<true>(g.out, stage, acc, m0, n0, n0 + kRun, lane);
       // every stage of this CTA's only tile has been read: its partial sums take their place
       else stage_part<TN>(smem, acc, row, col0, col0 + kRun);
     }

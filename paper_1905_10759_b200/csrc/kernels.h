@@ -247,6 +247,9 @@ cudaError_t launch_fp8_quantize(const void* x, bool x_bf16, int64_t rows, int64_
                                 int64_t ld_s, bool blocks, cudaStream_t stream);
 // C = A^ W^^T (transposed: C = A^ W^, the contraction along the rows of W).
 cudaError_t launch_fp8_gemm(const Fp8View& A, const Fp8View& W, bool transposed, void* C, bool c_bf16, int64_t ldc, cudaStream_t stream);
+// The same (not transposed) for few rows of A.
+bool fp8_gemv_supported(const Fp8View& A);
+cudaError_t launch_fp8_gemv(const Fp8View& A, const Fp8View& W, void* C, bool c_bf16, int64_t ldc, cudaStream_t stream);
 cudaError_t fp8_gemm_health(int op, int* value);
 cudaError_t fp8_weight_grad_health(int op, int* value);
 cudaError_t launch_fp8_weight_grad(const void* gy, int64_t N, int64_t ldg, const Fp8View& X, const float* base, int64_t ld_base, float* gw,
