@@ -64,17 +64,8 @@ __device__ __forceinline__ uint32_t scale_exponent(uint32_t amax_bits) {
 __device__ __forceinline__ float pow2_of(uint32_t exponent) { return __uint_as_float(exponent << 23); }
 __device__ __forceinline__ float pow2_inverse(uint32_t exponent) { return __uint_as_float((254u - exponent) << 23); }
 
-// Bits of |x| where x is finite, 0 where it is not.
-__device__ __forceinline__ uint32_t finite_magnitude(float x) {
-  const uint32_t b = __float_as_uint(x) & 0x7FFFFFFFu;
-  return b < 0x7F800000u ? b : 0u;
-}
-// x / s for the conversion: NaN for what is not finite; + 0 so that -0 leaves as +0 (a tiny negative product rounds to -0 and
-// keeps its sign bit).
-__device__ __forceinline__ float scaled(float x, float inverse) {
-  const float v = fmaf(x, inverse, 0.0f);
-  return (__float_as_uint(x) & 0x7F800000u) == 0x7F800000u ? __uint_as_float(0x7FC00000u) : v;
-}
+// x / s for the conversion; + 0 so that -0 leaves as +0 (a tiny negative product rounds to -0 and keeps its sign bit).
+__device__ __forceinline__ float scaled(float x, float inverse) { return fmaf(x, inverse, 0.0f); }
 
 }  // namespace fp8
 }  // namespace hbmm

@@ -23,7 +23,7 @@
 //   warps 12-15 : scouts: look the scales over and write their exponents to tensor memory
 // What both CTAs have to know (their scales' kind) goes as asynchronous stores that complete on the barrier the readers wait at; the
 // arrivals across the pair release nothing but reads.  (Store and releasing arrival: 2600 clk beside the copies, 0.53 ms.)
-// Products of few tiles: a cluster of two or four pairs shares each tile in equal parts of K (fp8_tile.cuh).
+// Products of few tiles: a cluster of two to four pairs shares each tile in equal parts of K (fp8_tile.cuh).
 #include <cuda_bf16.h>
 #include "fp8_tile.cuh"
 #include "kernels.h"
@@ -52,7 +52,6 @@ constexpr int OFF_A = 0, OFF_B = STAGES * kTile, OFF_OUT = STAGES * STAGE, OFF_S
 constexpr int OFF_BAR = OFF_SCALES + kSlots * kSlotBytes;
 constexpr int kBars = 2 * STAGES + 2 * kUnits + 2 + 3 * kSlots + 1;
 constexpr int OFF_FLAGS = OFF_BAR + kBars * 8, kBytes = OFF_FLAGS + kSlots * 8 + 16;
-constexpr int kMostParts = 4;                  // pairs that share a tile
 static_assert(kBytes <= 227 * 1024 && TM * TN * 4 <= STAGES * STAGE && kFactorCols + kSlots * kFactorSlot <= 512, "shared and tensor memory");
 
 struct Args {
@@ -441,7 +440,7 @@ fp8_gemm_kernel(const Args g, const __grid_constant__ CUtensorMap a_map, const _
     if (warp < kEpilogueWarps) {
       int64_t tm, tn;
       tile_at(walker, tiles_m, tiles_n, &tm, &tn);
-      finish_parts<TN, kMostParts>(g.out, smem, part, g.parts, half, tm * 2 * TM + half * TM, tn * TN, tid, kEpilogueWarps * 32);
+      finish_parts<TN>(g.out, smem, part, g.parts, half, tm * 2 * TM + half * TM, tn * TN, tid, kEpilogueWarps * 32);
     }
     __syncwarp();
   }
@@ -468,13 +467,7 @@ bool make_map(const Fp8View& v, CUtensorMap* map) {
             CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-// Pairs per tile: as many (1, 2, 4) as the machine holds at once, a step at least for each.
-int choose_parts(int64_t tiles, int64_t pairs, int groups) {
-  const int steps = (groups + kStep - 1) / kStep;
-  int parts = 1;
-  while (parts < kMostParts && tiles * parts * 2 <= pairs && steps >= parts * 2) parts *= 2;
-  return parts;
-}
+std::atomic<int> g_resident[64][kMostParts + 1];          // per device; both instantiations take a whole SM per CTA
 
 template <bool TRANS>
 cudaError_t launch(Args g, const Fp8View& A, const Fp8View& W, int dev, int sms, cudaStream_t stream) {
@@ -487,7 +480,7 @@ cudaError_t launch(Args g, const Fp8View& A, const Fp8View& W, int dev, int sms,
   CUtensorMap a_map, w_map;
   if (!make_map(A, &a_map) || !make_map(W, &w_map)) return cudaErrorNotSupported;
   const int64_t tiles = ((g.out.M + 2 * TM - 1) / (2 * TM)) * ((g.out.N + TN - 1) / TN), pairs = sms / 2;
-  g.parts = choose_parts(tiles, pairs, g.groups);
+  g.parts = dev >= 0 && dev < 64 ? choose_parts(fp8_gemm_kernel<TRANS>, kThreads, kBytes, g_resident[dev], tiles, pairs, (g.groups + kStep - 1) / kStep, 1) : 1;
   const int64_t clusters = g.parts > 1 ? tiles : (tiles < pairs ? tiles : pairs);
   return launch_pdl_cluster(fp8_gemm_kernel<TRANS>, dim3(static_cast<unsigned>(clusters * 2 * g.parts)), dim3(kThreads),
                             static_cast<unsigned>(2 * g.parts), kBytes, stream, g, a_map, w_map);

@@ -66,6 +66,22 @@ __device__ __forceinline__ void store_codes(uint8_t* row, int64_t k, int64_t K, 
   }
 }
 
+// Largest magnitude that is no NaN (infinite where an element is).
+template <int EPT>
+__device__ __forceinline__ float largest(const float (&v)[EPT]) {
+  float top = 0.0f;
+#pragma unroll
+  for (int e = 0; e < EPT; e++) top = fmaxf(top, fabsf(v[e]));
+  return top;
+}
+// An infinity counts as NaN does: as no number.  (A group's maximum shows whether it holds one, so that most groups skip this.)
+template <int EPT>
+__device__ __forceinline__ void drop_infinities(float (&v)[EPT]) {
+#pragma unroll
+  for (int e = 0; e < EPT; e++)
+    if (isinf(v[e])) v[e] = __uint_as_float(0x7FC00000u);
+}
+
 template <bool BF16, bool VEC>
 __global__ void __launch_bounds__(kThreads)
 fp8_quantize_rows(const void* x, int64_t rows, int64_t K, int64_t ldx, uint8_t* codes, int64_t ld, float* scales, int64_t ld_s) {
@@ -82,11 +98,18 @@ fp8_quantize_rows(const void* x, int64_t rows, int64_t K, int64_t ldx, uint8_t* 
     for (int j = 0; j < LOADS; j++) load_run<BF16, EPT, VEC>(row, k0 + j * PER_LOAD, K, v[j]);
 #pragma unroll
     for (int j = 0; j < LOADS; j++) {
-      uint32_t top = 0;
+      const auto group_top = [&] {                      // magnitudes order as their bits do
+        uint32_t top = __float_as_uint(largest<EPT>(v[j]));
+        if constexpr (LANES == 32) return __reduce_max_sync(0xffffffffu, top);
 #pragma unroll
-      for (int e = 0; e < EPT; e++) top = max(top, finite_magnitude(v[j][e]));
-#pragma unroll
-      for (int off = 1; off < LANES; off <<= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, off));
+        for (int off = 1; off < LANES; off <<= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, off));
+        return top;
+      };
+      uint32_t top = group_top();
+      if (__any_sync(0xffffffffu, top >= 0x7F800000u)) {
+        drop_infinities<EPT>(v[j]);
+        top = group_top();
+      }
       const uint32_t ex = scale_exponent(top);
       const int64_t k = k0 + j * PER_LOAD;
       if (k < K) {
@@ -101,7 +124,7 @@ template <bool BF16, bool VEC>
 __global__ void __launch_bounds__(kThreads)
 fp8_quantize_blocks(const void* x, int64_t rows, int64_t K, int64_t ldx, uint8_t* codes, int64_t ld, float* scales, int64_t ld_s) {
   constexpr int WARPS = kThreads / 32, PER_WARP = kGroup / WARPS;      // a warp's 16 rows, four elements per lane and row
-  __shared__ uint32_t tops[WARPS];
+  __shared__ uint32_t tops[2][WARPS];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   pdl_wait();
   const int64_t G = (K + kGroup - 1) / kGroup, items = (rows + kGroup - 1) / kGroup * G;
@@ -111,22 +134,30 @@ fp8_quantize_blocks(const void* x, int64_t rows, int64_t K, int64_t ldx, uint8_t
 #pragma unroll
     for (int i = 0; i < PER_WARP; i++)
       load_run<BF16, 4, VEC>(static_cast<const char*>(x) + (r0 + i) * ldx * (BF16 ? 2 : 4), k, r0 + i < rows ? K : 0, v[i]);
-    uint32_t top = 0;
+    const auto block_top = [&](int at) {
+      float top = 0.0f;
 #pragma unroll
-    for (int i = 0; i < PER_WARP; i++)
+      for (int i = 0; i < PER_WARP; i++) top = fmaxf(top, largest<4>(v[i]));
+      const uint32_t bits = __reduce_max_sync(0xffffffffu, __float_as_uint(top));
+      if (lane == 0) tops[at][warp] = bits;
+      __syncthreads();
+      uint32_t all = 0;
 #pragma unroll
-      for (int e = 0; e < 4; e++) top = max(top, finite_magnitude(v[i][e]));
-    top = __reduce_max_sync(0xffffffffu, top);
-    __syncthreads();                                    // the previous block's maxima have been read
-    if (lane == 0) tops[warp] = top;
-    __syncthreads();
+      for (int w = 0; w < WARPS; w++) all = max(all, tops[at][w]);
+      return all;
+    };
+    uint32_t top = block_top(0);
+    if (top >= 0x7F800000u) {                           // the same in every thread
 #pragma unroll
-    for (int w = 0; w < WARPS; w++) top = max(top, tops[w]);
+      for (int i = 0; i < PER_WARP; i++) drop_infinities<4>(v[i]);
+      top = block_top(1);
+    }
     const uint32_t ex = scale_exponent(top);
 #pragma unroll
     for (int i = 0; i < PER_WARP; i++)
       if (r0 + i < rows && k < K) store_codes<4>(codes + (r0 + i) * ld, k, K, v[i], pow2_inverse(ex));
     if (threadIdx.x == 0) scales[br * ld_s + g] = pow2_of(ex);
+    __syncthreads();                                    // every thread has read the maxima
   }
 }
 

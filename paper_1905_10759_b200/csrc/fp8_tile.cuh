@@ -2,6 +2,7 @@
 // registers (one row per thread), finished tiles leave through shared memory in whole lines, and the parts of a tile that several
 // CTA pairs of a cluster share are added over distributed shared memory in rank order (no atomics: the same sum in every run).
 #pragma once
+#include <atomic>
 #include <cuda_bf16.h>
 #include "fp8_common.cuh"
 #include "umma_common.cuh"
@@ -167,6 +168,7 @@ __device__ __forceinline__ void store_tile(const Out& o, unsigned char* stage, c
 }
 
 // ---- tiles shared by several CTAs of a cluster
+constexpr int kMostParts = 4;                 // pairs of a cluster that may share a tile
 // The 16-byte piece u of a row of TN fp32 partial sums.
 template <int TN>
 __device__ __forceinline__ int part_offset(int row, int u) { return row * (TN * 4) + ((u ^ (row & 7)) << 4); }
@@ -188,7 +190,7 @@ __device__ __forceinline__ float4 ld_cluster16(uint32_t addr) {
   return v;
 }
 // This CTA's share (part `mine` of `parts`) of the 128 rows of a tile whose partial sums lie in the CTAs `rank0`, `rank0` + 2, ...
-template <int TN, int MOST>
+template <int TN>
 __device__ __forceinline__ void finish_parts(const Out& o, unsigned char* base, int mine, int parts, uint32_t rank0, int64_t m0, int64_t n0, int tid,
                                              int threads) {
   const int r0 = mine * TM / parts, r1 = (mine + 1) * TM / parts;
@@ -196,16 +198,49 @@ __device__ __forceinline__ void finish_parts(const Out& o, unsigned char* base, 
     const int row = r0 + i / (TN / 4), u = i % (TN / 4);
     if (m0 + row >= o.M || n0 + 4 * u >= o.N) continue;
     const uint32_t at = smem_u32(base + part_offset<TN>(row, u));
-    float4 v[MOST];
+    float4 v[kMostParts];
 #pragma unroll
-    for (int q = 0; q < MOST; q++)
+    for (int q = 0; q < kMostParts; q++)
       if (q < parts) v[q] = ld_cluster16(mapa_rank(at, rank0 + 2 * q));
     float4 sum = v[0];
 #pragma unroll
-    for (int q = 1; q < MOST; q++)
+    for (int q = 1; q < kMostParts; q++)
       if (q < parts) { sum.x += v[q].x; sum.y += v[q].y; sum.z += v[q].z; sum.w += v[q].w; }
     store_out4(o, m0 + row, n0 + 4 * u, sum);
   }
+}
+
+// How many pairs (one cluster) share a tile: as many, up to four, as leave every tile's cluster resident at once (a B200 with 74 pairs
+// holds 33 clusters of two, 22 of three and 15 of four pairs of such CTAs; 16 tiles in clusters of four took twice the time of one
+// turn) and each at least `least` of a tile's `units` of the contraction.  known: what the device answered before, plus one; a
+// failure is not kept and costs this call the split.
+template <typename Kernel>
+int choose_parts(Kernel kernel, int threads, int bytes, std::atomic<int> (&known)[kMostParts + 1], int64_t tiles, int64_t pairs, int units, int least) {
+  for (int parts = kMostParts; parts >= 2; parts--) {
+    if (tiles * parts > pairs || units < parts * least) continue;
+    int n = known[parts].load(std::memory_order_relaxed);
+    if (n == 0) {
+      cudaLaunchConfig_t cfg = {};
+      cfg.gridDim = dim3(static_cast<unsigned>(2 * parts * pairs));
+      cfg.blockDim = dim3(static_cast<unsigned>(threads));
+      cfg.dynamicSmemBytes = static_cast<size_t>(bytes);
+      cudaLaunchAttribute attr[1];
+      attr[0].id = cudaLaunchAttributeClusterDimension;
+      attr[0].val.clusterDim.x = static_cast<unsigned>(2 * parts);
+      attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+      cfg.attrs = attr;
+      cfg.numAttrs = 1;
+      int clusters = 0;
+      if (cudaOccupancyMaxActiveClusters(&clusters, kernel, &cfg) != cudaSuccess) {
+        cudaGetLastError();                             // this answer's failure is not the launch's
+        continue;
+      }
+      n = clusters + 1;
+      known[parts].store(n, std::memory_order_relaxed);
+    }
+    if (tiles <= n - 1) return parts;
+  }
+  return 1;
 }
 
 // Output tiles are walked in blocks of eight rows of tiles, column by column, so that the tiles in flight at one time cover about as

@@ -13,7 +13,7 @@
 //   warps 0-7   : epilogue (TMEM lanes 32 * (w % 4).., columns 128 * (w / 4)..)
 //   warp  8     : this CTA's copies;  warp 9 : TMEM allocation, MMA issue in the first CTA;  warp 10 : scales, up to 16 stages ahead
 //   warps 12-19 : converters
-// Few tiles: a cluster of two or four pairs shares each tile in equal parts of m (fp8_tile.cuh).
+// Few tiles: a cluster of two to four pairs shares each tile in equal parts of m (fp8_tile.cuh).
 #include <cuda_bf16.h>
 #include "fp8_tile.cuh"
 #include "kernels.h"
@@ -34,7 +34,6 @@ constexpr int OFF_A = 0, OFF_B = STAGES * kOperand, OFF_CODES = 2 * STAGES * kOp
 constexpr int OFF_SCALES = OFF_OUT + kEpilogueWarps * kStoreBytes, OFF_BAR = OFF_SCALES + kSlots * ROWS * 4;
 constexpr int kBars = 4 * STAGES + 2 * kSlots + 5;
 constexpr int kBytes = OFF_BAR + kBars * 8 + 16;
-constexpr int kMostParts = 4;
 // An accumulator in tensor memory takes 512 rows, the epilogue adds it to fp32 registers: the tensor cores' additions truncate, always
 // towards zero, and with 8192 rows of sizes from 2^-8 to 2^8 in one accumulator the result was 9e-6 off.
 constexpr int kChunkStages = 512 / ROWS;
@@ -290,7 +289,7 @@ fp8_weight_grad_kernel(const Args g, const __grid_constant__ CUtensorMap gy_map,
     if (warp < kEpilogueWarps) {
       int64_t tm, tn;
       tile_at(walker, tiles_m, tiles_n, &tm, &tn);
-      finish_parts<TN, kMostParts>(g.out, smem, part, g.parts, half, tm * 2 * TM + half * TM, tn * TN, tid, kEpilogueWarps * 32);
+      finish_parts<TN>(g.out, smem, part, g.parts, half, tm * 2 * TM + half * TM, tn * TN, tid, kEpilogueWarps * 32);
     }
   }
   // No CTA may leave while another can still reach into it.
@@ -303,6 +302,8 @@ fp8_weight_grad_kernel(const Args g, const __grid_constant__ CUtensorMap gy_map,
     tmem_dealloc_pair(tmem_base, 512);
   }
 }
+
+std::atomic<int> g_resident[64][kMostParts + 1];          // per device
 
 bool make_map(const void* p, bool bf16, int64_t rows, int64_t cols, int64_t pitch, CUtensorMap* map) {
   EncodeTiledFn fn = encode_tiled_fn();
@@ -336,8 +337,7 @@ cudaError_t launch_fp8_weight_grad(const void* gy, int64_t N, int64_t ldg, const
   g.rows = X.rows;
   g.stages = static_cast<int32_t>((X.rows + ROWS - 1) / ROWS);
   const int64_t tiles = ((N + 2 * TM - 1) / (2 * TM)) * ((X.K + TN - 1) / TN), pairs = sms / 2;
-  g.parts = 1;
-  while (g.parts < kMostParts && tiles * g.parts * 2 <= pairs && g.stages >= g.parts * 2 * 2) g.parts *= 2;
+  g.parts = dev >= 0 && dev < 64 ? choose_parts(fp8_weight_grad_kernel, kThreads, kBytes, g_resident[dev], tiles, pairs, g.stages, 2) : 1;
   const int64_t clusters = g.parts > 1 ? tiles : (tiles < pairs ? tiles : pairs);
   return launch_pdl_cluster(fp8_weight_grad_kernel, dim3(static_cast<unsigned>(clusters * 2 * g.parts)), dim3(kThreads), static_cast<unsigned>(2 * g.parts),
                             kBytes, stream, g, gy_map, x_map);
