@@ -10,7 +10,6 @@
 #include "fp8_common.cuh"
 #include "kernels.h"
 #include "pdl.cuh"
-#include "row_io.cuh"
 
 namespace hbmm {
 namespace {
@@ -18,6 +17,7 @@ namespace {
 using namespace fp8;
 
 constexpr int kThreads = 256;
+constexpr int kResident = 4;          // CTAs per SM of the walk below (64 registers a thread)
 
 struct BackArgs {
   const uint8_t* codes; const float* scales;
@@ -34,52 +34,88 @@ template <> __device__ __forceinline__ __nv_bfloat16 rounded<__nv_bfloat16>(floa
 // Elements per lane.
 template <typename T> struct Per { static constexpr int N = 16 / sizeof(T); };
 
+// What a lane reads of a run: codes, gradients (raw), the run's scale.
+template <int E> struct Item { uint32_t c[E / 4]; uint4 g; float scale; };
+
+// The largest magnitude of a code whose product with the scale is at most 1 in fp32: [|x^| <= 1] is one comparison of the code's own
+// value.  A power of two: its inverse.
+__device__ __forceinline__ float clip_limit(float scale) {
+  const uint32_t bits = __float_as_uint(scale);
+  if ((bits & 0x807FFFFFu) == 0 && bits - 0x00800000u < 0x7E000000u) return __uint_as_float((254u << 23) - bits);
+  const uint32_t code = to_e4m3x2(1.0f / scale, 0.0f) & 0x7Fu;        // nearest; the one below where that is too large
+  const float v = from_e4m3x2(code).x;
+  return v * scale > 1.0f && code != 0 ? from_e4m3x2(code - 1).x : v;
+}
+
 template <typename T, int BETA, bool VEC>
 __global__ void __launch_bounds__(kThreads)
 fp8_binarize_backward_rows(const BackArgs a) {
   constexpr int E = Per<T>::N, RUN = 32 * E;                         // a warp's run: one scale group (fp32) or two (bf16)
   constexpr int IN = BETA < E ? BETA : E, LANES = BETA > E ? BETA / E : 1;
+  constexpr bool BF16 = E == 8;
   pdl_wait();
   const int lane = threadIdx.x & 31;
-  const int64_t chunks = (a.K + RUN - 1) / RUN, items = a.rows * chunks;
-  const int64_t nwarps = static_cast<int64_t>(gridDim.x) * (kThreads / 32);
-  for (int64_t it = (static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x) >> 5; it < items; it += nwarps) {    // warp-uniform
-    const int64_t r = it / chunks, k = (it - r * chunks) * RUN + lane * E;
+  RowWalk ahead((static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x) >> 5, static_cast<int64_t>(gridDim.x) * (kThreads / 32),
+                (a.K + RUN - 1) / RUN);                              // of a warp
+  const auto fetch = [&](Item<E>& l) {
+    const int64_t r = ahead.row, k = ahead.chunk * RUN + lane * E;
     const T* gy = static_cast<const T*>(a.gy) + r * a.ldg;
-    T* gx = static_cast<T*>(a.gx) + r * a.ldo;
     const uint8_t* codes = a.codes + r * a.ld;
+    l.scale = k < a.K ? loadf(a.scales + r * a.ld_s + k / kGroup) : 0.0f;
     const bool whole = k + E <= a.K;
-    uint32_t c[E / 4] = {};
-    float g[E];
-    const float scale = k < a.K ? loadf(a.scales + r * a.ld_s + k / kGroup) : 0.0f;
     if (whole) {                                                     // codes start on 16 bytes and k is a multiple of E
-      if constexpr (E == 8) { const uint2 q = load8(codes + k); c[0] = q.x; c[1] = q.y; }
-      else c[0] = load4(codes + k);
+      if constexpr (BF16) { const uint2 q = load8(codes + k); l.c[0] = q.x; l.c[1] = q.y; }
+      else l.c[0] = load4(codes + k);
     } else {
+#pragma unroll
+      for (int e = 0; e < E / 4; e++) l.c[e] = 0;
 #pragma unroll
       for (int e = 0; e < E; e++)
-        if (k + e < a.K) c[e / 4] |= load1(codes + k + e) << (8 * (e % 4));
+        if (k + e < a.K) l.c[e / 4] |= load1(codes + k + e) << (8 * (e % 4));
     }
     if (VEC && whole) {
-      const uint4 q = load16(gy + k);
-      const uint32_t w[4] = {q.x, q.y, q.z, q.w};
-#pragma unroll
-      for (int i = 0; i < 4; i++) {
-        if constexpr (E == 8) { g[2 * i] = __uint_as_float(w[i] << 16); g[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u); }
-        else g[i] = __uint_as_float(w[i]);
-      }
+      l.g = load16(gy + k);
     } else {
+      uint32_t w[4] = {0, 0, 0, 0};
 #pragma unroll
-      for (int e = 0; e < E; e++) g[e] = k + e < a.K ? load_elem<T>(gy + k + e) : 0.0f;
+      for (int e = 0; e < E; e++)
+        if (k + e < a.K) {
+          const uint32_t v = __float_as_uint(load_elem<T>(gy + k + e));
+          if constexpr (BF16) w[e / 2] |= e % 2 ? v : v >> 16;
+          else w[e] = v;
+        }
+      l.g = make_uint4(w[0], w[1], w[2], w[3]);
     }
-    float mag[E], back[E];                                           // |x^| and gy s
+  };
+  Item<E> next;
+  if (ahead.row < a.rows) fetch(next);
+  while (ahead.row < a.rows) {
+    const Item<E> l = next;
+    const int64_t r = ahead.row, k0 = ahead.chunk * RUN, k = k0 + lane * E;
+    ahead.next();
+    if (ahead.row < a.rows) fetch(next);                             // in flight while this one is worked on
+    const uint32_t gw[4] = {l.g.x, l.g.y, l.g.z, l.g.w};
+    float mag[E], back[E];                                           // the code's magnitude (without its scale) and gy s
+    uint32_t sign[4];                                                // the signs where gw's are
 #pragma unroll
     for (int e = 0; e < E; e += 2) {
-      const float2 f = from_e4m3x2((c[e / 4] & 0x7F7F7F7Fu) >> (8 * (e % 4)));
-      mag[e] = f.x * scale; mag[e + 1] = f.y * scale;
+      const float2 f = from_e4m3x2((l.c[e / 4] & 0x7F7F7F7Fu) >> (8 * (e % 4)) & 0xFFFFu);
+      mag[e] = f.x; mag[e + 1] = f.y;
     }
 #pragma unroll
-    for (int e = 0; e < E; e++) back[e] = with_sign(g[e], c[e / 4] >> (8 * (e % 4)));
+    for (int i = 0; i < 4; i++) {
+      if constexpr (BF16) {
+        sign[i] = __byte_perm(l.c[i / 2], 0u, i % 2 ? 0x3424 : 0x1404) & 0x80008000u;
+        const uint32_t w = gw[i] ^ sign[i];
+        back[2 * i] = __uint_as_float(w << 16);
+        back[2 * i + 1] = __uint_as_float(w & 0xFFFF0000u);
+      } else {
+        sign[i] = l.c[0] << (24 - 8 * i) & 0x80000000u;
+        back[i] = __uint_as_float(gw[i] ^ sign[i]);
+      }
+    }
+    const float limit = clip_limit(l.scale);
+    const bool inside = k0 + RUN <= a.K;                             // warp-uniform: every group of the run is whole or ends with it
     float o[E];
 #pragma unroll
     for (int q = 0; q < E; q += IN) {                                // the groups of this lane
@@ -96,24 +132,32 @@ fp8_binarize_backward_rows(const BackArgs a) {
         sm += __shfl_xor_sync(0xffffffffu, sm, off);
         sb += __shfl_xor_sync(0xffffffffu, sb, off);
       }
-      const int64_t left = a.K - (k + q) / BETA * BETA;              // elements from the group's start on
       float dm, db;
-      if (left >= BETA) { dm = sm * (1.0f / BETA); db = sb * (1.0f / BETA); }
-      else { const float n = static_cast<float>(left > 0 ? left : 1); dm = sm / n; db = sb / n; }
-#pragma unroll
-      for (int e = q; e < q + IN; e++) o[e] = with_sign(db, c[e / 4] >> (8 * (e % 4))) + (mag[e] <= 1.0f ? dm * g[e] : 0.0f);
-    }
-    if (VEC && whole) {
-      if constexpr (E == 8) {
-        *reinterpret_cast<uint4*>(gx + k) = make_uint4(rowio::bf16_pair(o[0], o[1]), rowio::bf16_pair(o[2], o[3]),
-                                                       rowio::bf16_pair(o[4], o[5]), rowio::bf16_pair(o[6], o[7]));
+      sm *= l.scale;                                                 // one scale: a group lies in one run of 128
+      if (inside) {
+        dm = sm * (1.0f / BETA); db = sb * (1.0f / BETA);
       } else {
-        *reinterpret_cast<float4*>(gx + k) = make_float4(o[0], o[1], o[2], o[3]);
+        const int64_t left = a.K - (k + q) / BETA * BETA;            // elements from the group's start on
+        const float n = static_cast<float>(left >= BETA ? BETA : left > 0 ? left : 1);
+        dm = sm / n; db = sb / n;
       }
+      // s db + delta gy = s (db + delta gy s)
+#pragma unroll
+      for (int e = q; e < q + IN; e++) o[e] = db + (mag[e] <= limit ? dm * back[e] : 0.0f);
+    }
+    T* gx = static_cast<T*>(a.gx) + r * a.ldo;
+    uint32_t w[4];
+#pragma unroll
+    for (int i = 0; i < 4; i++) w[i] = (BF16 ? bf16x2(o[2 * i % E], o[(2 * i + 1) % E]) : __float_as_uint(o[i])) ^ sign[i];
+    if (VEC && k + E <= a.K) {
+      *reinterpret_cast<uint4*>(gx + k) = make_uint4(w[0], w[1], w[2], w[3]);
     } else {
 #pragma unroll
       for (int e = 0; e < E; e++)
-        if (k + e < a.K) gx[k + e] = rounded<T>(o[e]);
+        if (k + e < a.K) {
+          if constexpr (BF16) reinterpret_cast<unsigned short*>(gx)[k + e] = static_cast<unsigned short>(w[e / 2] >> (16 * (e % 2)));
+          else reinterpret_cast<uint32_t*>(gx)[k + e] = w[e];
+        }
     }
   }
 }
@@ -171,15 +215,14 @@ fp8_binarize_backward_teams(const BackArgs a, int64_t beta) {
 
 template <typename T>
 cudaError_t launch(const BackArgs& a, int64_t beta, int sms, cudaStream_t stream) {
-  const int64_t cap = static_cast<int64_t>(sms) * 32;
-  const auto grid = [&](int64_t work, int64_t per) {
-    const int64_t n = (work + per - 1) / per;
+  const auto grid = [&](int64_t work, int64_t per, int ctas = 32) {
+    const int64_t n = (work + per - 1) / per, cap = static_cast<int64_t>(sms) * ctas;
     return dim3(static_cast<unsigned>(n < cap ? n : cap));
   };
   // group sizes a warp takes by shuffles (a row shorter than its group has a last group of its own length like any other)
   if ((beta & (beta - 1)) == 0 && beta <= 128) {
     const int64_t run = 32 * Per<T>::N;
-    const dim3 g = grid(a.rows * ((a.K + run - 1) / run), kThreads / 32);
+    const dim3 g = grid(a.rows * ((a.K + run - 1) / run), kThreads / 32, kResident);     // all at once: a warp reads ahead along its walk
     const bool vec = reinterpret_cast<uintptr_t>(a.gy) % 16 == 0 && reinterpret_cast<uintptr_t>(a.gx) % 16 == 0 &&
                      a.ldg * static_cast<int64_t>(sizeof(T)) % 16 == 0 && a.ldo * static_cast<int64_t>(sizeof(T)) % 16 == 0;
 #define HBMM_B(B)                                                                                                                   \

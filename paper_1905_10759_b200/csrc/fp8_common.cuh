@@ -32,6 +32,20 @@ __device__ __forceinline__ uint32_t load1(const void* p) {
 }
 __device__ __forceinline__ float loadf(const float* p) { return __uint_as_float(load4(p)); }
 
+// A walk over the (row, chunk) pairs of a matrix, row by row, `step` pairs at a time: without the division per turn that the pair's
+// number would take (64-bit, 80 instructions; a third of what the quantizer executed).
+struct RowWalk {
+  int64_t row, chunk, chunks, step_rows, step_chunks;
+  __device__ __forceinline__ RowWalk(int64_t first, int64_t step, int64_t chunks_) : chunks(chunks_) {
+    row = first / chunks; chunk = first - row * chunks;
+    step_rows = step / chunks; step_chunks = step - step_rows * chunks;
+  }
+  __device__ __forceinline__ void next() {
+    row += step_rows; chunk += step_chunks;
+    if (chunk >= chunks) { chunk -= chunks; row++; }
+  }
+};
+
 // Two fp32 -> two codes (lo in the low byte), nearest even; magnitudes above 448 saturate, NaN gives the NaN code.
 __device__ __forceinline__ uint32_t to_e4m3x2(float lo, float hi) {
   unsigned short r;
