@@ -480,7 +480,7 @@ cudaError_t launch(Args g, const Fp8View& A, const Fp8View& W, int dev, int sms,
   CUtensorMap a_map, w_map;
   if (!make_map(A, &a_map) || !make_map(W, &w_map)) return cudaErrorNotSupported;
   const int64_t tiles = ((g.out.M + 2 * TM - 1) / (2 * TM)) * ((g.out.N + TN - 1) / TN), pairs = sms / 2;
-  g.parts = dev >= 0 && dev < 64 ? choose_parts(fp8_gemm_kernel<TRANS>, kThreads, kBytes, g_resident[dev], tiles, pairs, (g.groups + kStep - 1) / kStep, 1) : 1;
+  g.parts = dev >= 0 && dev < 64 ? choose_parts(fp8_gemm_kernel<TRANS>, kThreads, kBytes, g_resident[dev], tiles, pairs, (g.groups + kStep - 1) / kStep, 2) : 1;
   const int64_t clusters = g.parts > 1 ? tiles : (tiles < pairs ? tiles : pairs);
   return launch_pdl_cluster(fp8_gemm_kernel<TRANS>, dim3(static_cast<unsigned>(clusters * 2 * g.parts)), dim3(kThreads),
                             static_cast<unsigned>(2 * g.parts), kBytes, stream, g, a_map, w_map);

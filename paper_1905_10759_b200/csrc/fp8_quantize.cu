@@ -118,10 +118,13 @@ fp8_quantize_rows(const void* x, int64_t rows, int64_t K, int64_t ldx, uint8_t* 
     for (int j = 0; j < kLoads; j++) v[j] = load_raw<BF16, VEC>(row, k0 + j * PER_LOAD, K);
   };
   const auto over_group = [&](uint32_t top) {
-    if constexpr (LANES == 32) return __reduce_max_sync(0xffffffffu, top);
+    if constexpr (LANES == 32) {
+      return __reduce_max_sync(0xffffffffu, top);
+    } else {
 #pragma unroll
-    for (int off = 1; off < LANES; off <<= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, off));
-    return top;
+      for (int off = 1; off < LANES; off <<= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, off));
+      return top;
+    }
   };
   if (ahead.row < rows) fetch(next);
   while (ahead.row < rows) {

@@ -82,11 +82,12 @@ __device__ __forceinline__ void store_out4(const Out& o, int64_t m, int64_t n, f
   if (n + 2 < o.N) p[2] = v.z;
 }
 
-// A warp's 32 rows (row m0 + lane in this lane's registers) of the runs at columns n0 and n1 to memory, 16 columns at a time through
-// 2 KB of shared memory: lanes write their own rows and read eight rows of 64 bytes (32 columns in bf16), so that a store instruction fills whole sectors.
-// Pieces of 16 bytes lie at piece ^ (row / 2 % 4): no bank conflicts either way.  A block that lies inside the matrix goes without
-// checks, its base (if any) 16 columns ahead of its use: 32 loads one after another took 26 us per tile.
-constexpr int kStoreBytes = 2048;
+// A warp's 32 rows (row m0 + lane in this lane's registers) of the runs at columns n0 and n1 to memory through shared memory: lanes write
+// their own rows and read the rows of a store instruction side by side.  Pieces of 16 bytes lie where neither conflicts.
+//   narrow: eight rows of 64 bytes at a time, 16 columns in fp32, 32 in bf16 (rounded on the way in);
+//   wide (fp32): 16 rows at a time, four rows of whole 128-byte lines per store, and the base, if any, half a step ahead of its use.
+// A block that lies inside the matrix goes without checks.
+constexpr int kStoreBytes = 2048;             // per warp
 __device__ __forceinline__ unsigned char* store_piece(unsigned char* stage, int row, int piece) { return stage + row * 64 + ((piece ^ (row >> 1 & 3)) << 4); }
 // The base's lines of a warp's 32 rows x 128 columns into L2, some time before store_tile reads them.
 __device__ __forceinline__ void prefetch_base(const Out& o, int64_t m0, int64_t n0, int lane) {
@@ -95,12 +96,12 @@ __device__ __forceinline__ void prefetch_base(const Out& o, int64_t m0, int64_t 
   for (int c = 0; c < 4; c++)
     if (n0 + c * 32 < o.N) asm volatile("prefetch.global.L2 [%0];" ::"l"(o.base + (m0 + lane) * o.ld_base + n0 + c * 32));
 }
-template <bool BASE>
+template <bool WIDE>
 __device__ __forceinline__ void store_tile(const Out& o, unsigned char* stage, const uint64_t (&acc)[kRun], int64_t m0, int64_t n0, int64_t n1, int lane) {
   const int sub = lane / 4, piece = lane % 4;
   const int64_t r0 = m0 + sub;
   const bool inside = m0 + 32 <= o.M && n0 + kRun <= o.N && n1 + kRun <= o.N;
-  if (!BASE && inside && o.bf16) {                      // 32 columns at a time, rounded on the way in
+  if (!WIDE && inside && o.bf16) {                      // 32 columns at a time, rounded on the way in
     __nv_bfloat16* out = static_cast<__nv_bfloat16*>(o.c) + r0 * o.ldc + n0 + piece * 8;
 #pragma unroll
     for (int c = 0; c < 4; c++) {
@@ -124,15 +125,52 @@ __device__ __forceinline__ void store_tile(const Out& o, unsigned char* stage, c
     }
     return;
   }
+  if (WIDE && inside && !o.bf16) {
+    const int sub8 = lane / 8, piece8 = lane % 8;
+    const int64_t r8 = m0 + sub8;
+    float* out = static_cast<float*>(o.c) + r8 * o.ldc + n0 + piece8 * 4;
+    const bool base = o.base != nullptr;
+    const float* from = base ? o.base + r8 * o.ld_base + n0 + piece8 * 4 : nullptr;
+    uint4 ahead[4];
+    if (base) {
+#pragma unroll
+      for (int i = 0; i < 4; i++) ahead[i] = load16(from + i * 4 * o.ld_base);
+    }
+#pragma unroll
+    for (int c = 0; c < 4; c++) {
+      const int64_t on = c == 1 ? n1 - n0 - 32 : 32;
+#pragma unroll
+      for (int hf = 0; hf < 2; hf++) {                  // 16 of the rows at a time
+        __syncwarp();
+        if (lane / 16 == hf) {
+#pragma unroll
+          for (int p = 0; p < 8; p++)
+            *reinterpret_cast<uint4*>(swz(stage, lane % 16, p)) =
+                make_uint4(static_cast<uint32_t>(acc[c * 16 + 2 * p]), static_cast<uint32_t>(acc[c * 16 + 2 * p] >> 32),
+                           static_cast<uint32_t>(acc[c * 16 + 2 * p + 1]), static_cast<uint32_t>(acc[c * 16 + 2 * p + 1] >> 32));
+        }
+        __syncwarp();
+#pragma unroll
+        for (int i = 0; i < 4; i++) {
+          float4 v = *reinterpret_cast<const float4*>(swz(stage, i * 4 + sub8, piece8));
+          if (base) {
+            v.x += __uint_as_float(ahead[i].x); v.y += __uint_as_float(ahead[i].y);
+            v.z += __uint_as_float(ahead[i].z); v.w += __uint_as_float(ahead[i].w);
+          }
+          *reinterpret_cast<float4*>(out + (hf * 4 + i) * 4 * o.ldc) = v;
+        }
+        if (base && (c < 3 || hf == 0)) {
+          if (hf == 1) from += on;
+#pragma unroll
+          for (int i = 0; i < 4; i++) ahead[i] = load16(from + ((1 - hf) * 4 + i) * 4 * o.ld_base);
+        }
+      }
+      out += on;
+    }
+    return;
+  }
   const bool plain = inside && !o.bf16;
   float* out = static_cast<float*>(o.c) + r0 * o.ldc + n0 + piece * 4;
-  const bool base = BASE && plain && o.base != nullptr;
-  const float* from = base ? o.base + r0 * o.ld_base + n0 + piece * 4 : nullptr;
-  uint4 ahead[4];
-  if (BASE && base) {
-#pragma unroll
-    for (int i = 0; i < 4; i++) ahead[i] = load16(from + i * 8 * o.ld_base);
-  }
 #pragma unroll
   for (int c = 0; c < 8; c++) {
     __syncwarp();                                       // the columns before have been read
@@ -142,23 +180,10 @@ __device__ __forceinline__ void store_tile(const Out& o, unsigned char* stage, c
           make_uint4(static_cast<uint32_t>(acc[c * 8 + 2 * p]), static_cast<uint32_t>(acc[c * 8 + 2 * p] >> 32),
                      static_cast<uint32_t>(acc[c * 8 + 2 * p + 1]), static_cast<uint32_t>(acc[c * 8 + 2 * p + 1] >> 32));
     __syncwarp();
-    if (plain) {
+    if (!WIDE && plain) {
 #pragma unroll
-      for (int i = 0; i < 4; i++) {
-        float4 v = *reinterpret_cast<const float4*>(store_piece(stage, i * 8 + sub, piece));
-        if (BASE && base) {
-          v.x += __uint_as_float(ahead[i].x); v.y += __uint_as_float(ahead[i].y);
-          v.z += __uint_as_float(ahead[i].z); v.w += __uint_as_float(ahead[i].w);
-        }
-        *reinterpret_cast<float4*>(out + i * 8 * o.ldc) = v;
-      }
-      const int64_t on = c == 3 ? n1 - n0 - kRun + 16 : 16;
-      out += on;
-      if (BASE && base && c < 7) {
-        from += on;
-#pragma unroll
-        for (int i = 0; i < 4; i++) ahead[i] = load16(from + i * 8 * o.ld_base);
-      }
+      for (int i = 0; i < 4; i++) *reinterpret_cast<float4*>(out + i * 8 * o.ldc) = *reinterpret_cast<const float4*>(store_piece(stage, i * 8 + sub, piece));
+      out += c == 3 ? n1 - n0 - kRun + 16 : 16;
     } else {
 #pragma unroll
       for (int i = 0; i < 4; i++)

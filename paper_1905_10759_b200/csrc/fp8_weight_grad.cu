@@ -337,7 +337,7 @@ cudaError_t launch_fp8_weight_grad(const void* gy, int64_t N, int64_t ldg, const
   g.rows = X.rows;
   g.stages = static_cast<int32_t>((X.rows + ROWS - 1) / ROWS);
   const int64_t tiles = ((N + 2 * TM - 1) / (2 * TM)) * ((X.K + TN - 1) / TN), pairs = sms / 2;
-  g.parts = dev >= 0 && dev < 64 ? choose_parts(fp8_weight_grad_kernel, kThreads, kBytes, g_resident[dev], tiles, pairs, g.stages, 2) : 1;
+  g.parts = dev >= 0 && dev < 64 ? choose_parts(fp8_weight_grad_kernel, kThreads, kBytes, g_resident[dev], tiles, pairs, g.stages, 4) : 1;
   const int64_t clusters = g.parts > 1 ? tiles : (tiles < pairs ? tiles : pairs);
   return launch_pdl_cluster(fp8_weight_grad_kernel, dim3(static_cast<unsigned>(clusters * 2 * g.parts)), dim3(kThreads), static_cast<unsigned>(2 * g.parts),
                             kBytes, stream, g, gy_map, x_map);
