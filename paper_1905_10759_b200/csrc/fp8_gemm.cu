@@ -47,10 +47,10 @@ constexpr int kStep = 4, kSlots = 8, kScalesA = 128 * kStep * 4, kSlotBytes = kS
 // A whole accumulator takes 16 steps (8192 elements) at most: the tensor cores' fp32 sums truncate, and the relative error of a result
 // grows with their number (256 x 256 outputs of K = 4096 / 8192: 7e-8 / 1.2e-7, 6e-8 / 7.5e-8 with a sum per group).
 constexpr int kChunk = 16;
-constexpr int kUnit = 128, kUnits = 3, kFactorCols = 384, kFactorSlot = 16;
+constexpr int kUnit = 128, kUnits = 3, kTurns = 2 * kUnits, kFactorCols = 384, kFactorSlot = 16;
 constexpr int OFF_A = 0, OFF_B = STAGES * kTile, OFF_OUT = STAGES * STAGE, OFF_SCALES = OFF_OUT + kEpilogueWarps * kStoreBytes;
 constexpr int OFF_BAR = OFF_SCALES + kSlots * kSlotBytes;
-constexpr int kBars = 2 * STAGES + 2 * kUnits + 2 + 3 * kSlots + 1;
+constexpr int kBars = 2 * STAGES + 2 * kTurns + 2 + 3 * kSlots + 1;
 constexpr int OFF_FLAGS = OFF_BAR + kBars * 8, kBytes = OFF_FLAGS + kSlots * 8 + 16;
 static_assert(kBytes <= 227 * 1024 && TM * TN * 4 <= STAGES * STAGE && kFactorCols + kSlots * kFactorSlot <= 512, "shared and tensor memory");
 
@@ -77,9 +77,11 @@ fp8_gemm_kernel(const Args g, const __grid_constant__ CUtensorMap a_map, const _
   extern __shared__ __align__(1024) unsigned char smem[];
   uint64_t* full = reinterpret_cast<uint64_t*>(smem + OFF_BAR);
   uint64_t* empty = full + STAGES;
-  uint64_t* ufull = empty + STAGES;            // units of partial sums
-  uint64_t* uempty = ufull + kUnits;
-  uint64_t* xfull = uempty + kUnits;           // the whole accumulator
+  // units of partial sums: partial sum i lies in unit i % 3, is read by warpgroup i % 2 and has barrier i % 6, so that a warpgroup
+  // meets a barrier of its own at its visits, one parity after the other
+  uint64_t* ufull = empty + STAGES;
+  uint64_t* uempty = ufull + kTurns;
+  uint64_t* xfull = uempty + kTurns;           // the whole accumulator
   uint64_t* xempty = xfull + 1;
   uint64_t* scales = xempty + 1;               // a step's scales are in this CTA's shared memory
   uint64_t* sfull = scales + kSlots;           // its factors are in both CTAs' tensor memory, and how it is summed is known
@@ -105,7 +107,7 @@ fp8_gemm_kernel(const Args g, const __grid_constant__ CUtensorMap a_map, const _
       mbar_init(&full[s], 1);           // first CTA: its loader's expect_tx arrival; the copies of both CTAs complete the bytes
       mbar_init(&empty[s], 1);          // MMA commit (to both CTAs)
     }
-    for (int u = 0; u < kUnits; u++) { mbar_init(&ufull[u], 1); mbar_init(&uempty[u], kEpilogueWarps); }    // one warpgroup of each CTA
+    for (int u = 0; u < kTurns; u++) { mbar_init(&ufull[u], 1); mbar_init(&uempty[u], kEpilogueWarps); }    // one warpgroup of each CTA
     mbar_init(xfull, 1);
     mbar_init(xempty, 2 * kEpilogueWarps);
     for (int f = 0; f < kSlots; f++) {
@@ -221,16 +223,16 @@ fp8_gemm_kernel(const Args g, const __grid_constant__ CUtensorMap a_map, const _
       const uint32_t full_a = smem_u32(full), empty_a = smem_u32(empty), ufull_a = smem_u32(ufull), uempty_a = smem_u32(uempty);
       const uint32_t sempty_a = smem_u32(sempty);
       uint32_t s = 0, full_par = 0;            // stage
-      uint32_t u = 0, u_round = 0;             // unit of the next partial sum, and how often the ring went round
+      uint32_t u = 0, u_round = 0;             // barrier of the next partial sum, and how often the ring of six went round
       uint32_t x = 0;                          // whole accumulators so far
       uint32_t f = 0, f_par = 0;               // slot of scales
       bool ok = true;
       // the accumulator's columns are free: the units' last partial sums and the last whole accumulator have been read
       const auto accumulator_free = [&] {
         if (x > 0 && !wait(smem_u32(xempty), (x & 1) ^ 1, 3)) return false;
-        for (uint32_t i = 0; i < 2; i++) {
+        for (uint32_t i = 0; i < kTurns; i++) {
           const uint32_t uses = u_round + (u > i ? 1 : 0);
-          if (uses > 0 && !wait(uempty_a + i * 8, (uses & 1) ^ 1, 3)) return false;
+          if (i % kUnits < 2 && uses > 0 && !wait(uempty_a + i * 8, (uses & 1) ^ 1, 3)) return false;
         }
         return true;
       };
@@ -267,16 +269,18 @@ fp8_gemm_kernel(const Args g, const __grid_constant__ CUtensorMap a_map, const _
             constexpr uint32_t idesc = instr_desc_pair(kUnit, kFmtE4M3) | kMajor;
             for (int j = 0; j < n && ok; j++) {
               for (uint32_t h = 0; h < 2; h++) {
-                if (u < 2 && x > 0 && !wait(smem_u32(xempty), (x & 1) ^ 1, 3)) { ok = false; break; }
-                if (u_round > 0 && !wait(uempty_a + u * 8, (u_round & 1) ^ 1, 3)) { ok = false; break; }
+                const uint32_t unit = u < kUnits ? u : u - kUnits, before = u < kUnits ? u + kUnits : u - kUnits;      // the unit's last sum
+                const uint32_t uses = u < kUnits ? u_round : u_round + 1;
+                if (unit < 2 && x > 0 && !wait(smem_u32(xempty), (x & 1) ^ 1, 3)) { ok = false; break; }
+                if (uses > 0 && !wait(uempty_a + before * 8, (uses & 1) ^ 1, 3)) { ok = false; break; }
                 if (h == 0 && !wait(full_a + s * 8, full_par, 2)) { ok = false; break; }
                 tc_fence_after();
                 const uint32_t a_lo = da_lo + s * (kTile >> 4), b_lo = db_lo + s * (kTile >> 4) + h * kHalfB;
 #pragma unroll
                 for (uint32_t ks = 0; ks < kGroup / 32; ks++)
-                  umma_f8_pair(tmem_base + u * kUnit, da_hi | (a_lo + ks * kStepA), db_hi | (b_lo + ks * kStepB), idesc, ks != 0 ? 1u : 0u);
+                  umma_f8_pair(tmem_base + unit * kUnit, da_hi | (a_lo + ks * kStepA), db_hi | (b_lo + ks * kStepB), idesc, ks != 0 ? 1u : 0u);
                 umma_commit_pair_mc(ufull_a + u * 8, both);
-                if (++u == kUnits) { u = 0; u_round++; }
+                if (++u == kTurns) { u = 0; u_round++; }
               }
               if (!ok) break;
               umma_commit_pair_mc(empty_a + s * 8, both);
@@ -366,7 +370,7 @@ fp8_gemm_kernel(const Args g, const __grid_constant__ CUtensorMap a_map, const _
     const uint32_t tmem_at = tmem_base + (static_cast<uint32_t>((warp & 3) * 32) << 16);
     const uint32_t uempty0 = mapa_rank(smem_u32(uempty), lead), xempty0 = mapa_rank(smem_u32(xempty), lead);
     unsigned char* stage = smem + OFF_OUT + warp * kStoreBytes;
-    uint32_t u = h, u_par = 0;                   // unit of this warpgroup's next partial sum: every second one is its own
+    uint32_t u = h, u_par = 0;                   // barrier of this warpgroup's next partial sum: every second one is its own
     uint32_t x_par = 0, f = 0, f_par = 0;
     uint64_t acc[kRun];
     bool ok = true;
@@ -405,13 +409,14 @@ fp8_gemm_kernel(const Args g, const __grid_constant__ CUtensorMap a_map, const _
             const float f0 = sa * w_scale<TRANS>(slot + kScalesA, 0, j), f1 = sa * w_scale<TRANS>(slot + kScalesA, 1, j);
             if (!wait(smem_u32(&ufull[u]), u_par, 5)) { ok = false; break; }
             tc_fence_after();
-            drain(tmem_at + u * kUnit, tmem_at + u * kUnit + 64, acc, f0, f1, [&] {
+            const uint32_t at = tmem_at + (u < kUnits ? u : u - kUnits) * kUnit;
+            drain(at, at + 64, acc, f0, f1, [&] {
               tc_fence_before();
               __syncwarp();
               if (lane == 0) mbar_arrive_cluster_read(uempty0 + u * 8);
             });
             u += 2;
-            if (u >= kUnits) { u -= kUnits; u_par ^= 1; }
+            if (u >= kTurns) { u -= kTurns; u_par ^= 1; }
           }
           if (!ok) break;
         }

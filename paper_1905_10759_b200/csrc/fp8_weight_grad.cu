@@ -32,7 +32,7 @@ constexpr int kChunkBytes = ROWS * 128;        // 64 columns of an operand: 128 
 constexpr int kSlots = 16;                     // stages of scales
 constexpr int OFF_A = 0, OFF_B = STAGES * kOperand, OFF_CODES = 2 * STAGES * kOperand, OFF_OUT = OFF_CODES + STAGES * kCodes;
 constexpr int OFF_SCALES = OFF_OUT + kEpilogueWarps * kStoreBytes, OFF_BAR = OFF_SCALES + kSlots * ROWS * 4;
-constexpr int kBars = 4 * STAGES + 2 * kSlots + 5;
+constexpr int kBars = 5 * STAGES + 2 * kSlots + 5;
 constexpr int kBytes = OFF_BAR + kBars * 8 + 16;
 // An accumulator in tensor memory takes 512 rows, the epilogue adds it to fp32 registers: the tensor cores' additions truncate, always
 // towards zero, and with 8192 rows of sizes from 2^-8 to 2^8 in one accumulator the result was 9e-6 off.
@@ -51,8 +51,10 @@ __global__ void __launch_bounds__(kThreads, 1)
 fp8_weight_grad_kernel(const Args g, const __grid_constant__ CUtensorMap gy_map, const __grid_constant__ CUtensorMap x_map) {
   extern __shared__ __align__(1024) unsigned char smem[];
   uint64_t* afull = reinterpret_cast<uint64_t*>(smem + OFF_BAR);     // first CTA: gy of both CTAs
-  uint64_t* cfull = afull + STAGES;            // this CTA's codes
-  uint64_t* bfull = cfull + STAGES;            // first CTA: converted, in both CTAs
+  // this CTA's codes: two barriers per stage, as two halves of the converters take turns and the number of stages is odd (with one,
+  // a half would wait for the same parity at every visit, and pass when the other half's codes have not come yet)
+  uint64_t* cfull = afull + STAGES;
+  uint64_t* bfull = cfull + 2 * STAGES;        // first CTA: converted, in both CTAs
   uint64_t* empty = bfull + STAGES;
   uint64_t* sfull = empty + STAGES;            // scales of a stage
   uint64_t* sempty = sfull + kSlots;
@@ -74,6 +76,7 @@ fp8_weight_grad_kernel(const Args g, const __grid_constant__ CUtensorMap gy_map,
     for (int s = 0; s < STAGES; s++) {
       mbar_init(&afull[s], 1);
       mbar_init(&cfull[s], 1);
+      mbar_init(&cfull[STAGES + s], 1);
       mbar_init(&bfull[s], kConvertWarps);                  // one half of the converters of each CTA
       mbar_init(&empty[s], 1);
     }
@@ -102,7 +105,7 @@ fp8_weight_grad_kernel(const Args g, const __grid_constant__ CUtensorMap gy_map,
       asm volatile("prefetch.tensormap [%0];" ::"l"(&gy_map) : "memory");
       asm volatile("prefetch.tensormap [%0];" ::"l"(&x_map) : "memory");
       const uint32_t afull0 = mapa_rank(smem_u32(afull), lead);
-      int s = 0;
+      int s = 0, c = 0;
       uint32_t par = 1;                                  // the first round waits for nobody
       int64_t issued = 0;
       bool ok = true;
@@ -113,8 +116,9 @@ fp8_weight_grad_kernel(const Args g, const __grid_constant__ CUtensorMap gy_map,
         for (int st = s0; st < s1; st++) {
           if (!wait(smem_u32(&empty[s]), par, 1)) { ok = false; break; }
           if (half == 0) mbar_arrive_expect_tx(&afull[s], 2 * kOperand);
-          mbar_arrive_expect_tx(&cfull[s], kCodes);
-          tma_load_2d(smem + OFF_CODES + s * kCodes, &x_map, k_at, st * ROWS, &cfull[s]);
+          mbar_arrive_expect_tx(&cfull[c], kCodes);
+          tma_load_2d(smem + OFF_CODES + s * kCodes, &x_map, k_at, st * ROWS, &cfull[c]);
+          if (++c == 2 * STAGES) c = 0;
           unsigned char* a = smem + OFF_A + s * kOperand;
           tma_load_2d_pair(a, &gy_map, n_at, st * ROWS, afull0 + s * 8);
           tma_load_2d_pair(a + kChunkBytes, &gy_map, n_at + 64, st * ROWS, afull0 + s * 8);
@@ -127,7 +131,7 @@ fp8_weight_grad_kernel(const Args g, const __grid_constant__ CUtensorMap gy_map,
         // barriers of its copies of gy and gives them a fixed time that is far longer than a copy)
         for (int64_t q = 1; q <= (issued < STAGES ? issued : STAGES); q++) {
           const int64_t i = issued - q;
-          mbar_wait_quiet(&cfull[i % STAGES], static_cast<uint32_t>((i / STAGES) & 1), kDrainPolls);
+          mbar_wait_quiet(&cfull[i % (2 * STAGES)], static_cast<uint32_t>((i / (2 * STAGES)) & 1), kDrainPolls);
           if (half == 0) mbar_wait_quiet(&afull[i % STAGES], static_cast<uint32_t>((i / STAGES) & 1), kDrainPolls);
         }
         if (half != 0)
@@ -165,12 +169,12 @@ fp8_weight_grad_kernel(const Args g, const __grid_constant__ CUtensorMap gy_map,
     const uint32_t mine = (warp - kConvertWarp) / 4;
     const uint32_t bfull0 = mapa_rank(smem_u32(bfull), lead);
     const int q = me & 7;                                // 16 codes from column 16 q, rows me / 8 + 16 i
-    uint32_t s = 0, par = 0, f = 0, f_par = 0, turn = 0;
+    uint32_t s = 0, c = 0, c_par = 0, f = 0, f_par = 0, turn = 0;
     bool ok = true;
     for (int64_t tile = walker; tile < n_tiles && ok; tile += walkers) {
       for (int st = s0; st < s1; st++, turn ^= 1) {
         if (turn == mine) {
-          if (!wait(smem_u32(&sfull[f]), f_par, 7) || !wait(smem_u32(&cfull[s]), par, 7)) { ok = false; break; }
+          if (!wait(smem_u32(&sfull[f]), f_par, 7) || !wait(smem_u32(&cfull[c]), c_par, 7)) { ok = false; break; }
           const float* scales = reinterpret_cast<const float*>(smem + OFF_SCALES + f * ROWS * 4) + (me >> 3);
           const unsigned char* codes = smem + OFF_CODES + s * kCodes + me * 16;
           // two 16-byte pieces of the row's 64 columns; lanes of the second 64 columns store theirs in the other order, so that the
@@ -181,9 +185,9 @@ fp8_weight_grad_kernel(const Args g, const __grid_constant__ CUtensorMap gy_map,
           unsigned char* to1 = swz(rows64, me >> 3, 2 * (q & 3) + (swap ? 0 : 1));
 #pragma unroll
           for (int i = 0; i < ROWS / 16; i++) {
-            const uint4 c = *reinterpret_cast<const uint4*>(codes + i * 16 * 128);
+            const uint4 x = *reinterpret_cast<const uint4*>(codes + i * 16 * 128);
             const float sc = scales[i * 16];
-            const uint32_t w[4] = {c.x, c.y, c.z, c.w};
+            const uint32_t w[4] = {x.x, x.y, x.z, x.w};
             uint32_t o[8];
 #pragma unroll
             for (int e = 0; e < 4; e++) {
@@ -201,7 +205,8 @@ fp8_weight_grad_kernel(const Args g, const __grid_constant__ CUtensorMap gy_map,
             mbar_arrive(&sempty[f]);
           }
         }
-        if (++s == STAGES) { s = 0; par ^= 1; }
+        if (++s == STAGES) s = 0;
+        if (++c == 2 * STAGES) { c = 0; c_par ^= 1; }
         if (++f == kSlots) { f = 0; f_par ^= 1; }
       }
     }

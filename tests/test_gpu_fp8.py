@@ -160,6 +160,26 @@ def test_weight_grad_of_many_tiles(hb, M, N, K, base):
     assert torch.equal(hb.fp8_weight_grad(gy, X, again, base=b), GW)
 
 
+@pytest.mark.parametrize("M,N,K", [(8192, 2304, 2304), (3000, 1024, 1024), (256, 4096, 2304)])
+def test_weight_grad_again_and_again(hb, M, N, K):
+    """The same bits every time, with the operands in L2 and with other data in their place."""
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(N)
+    X = hb.fp8_quantize(torch.randn(M, K, generator=gen, device="cuda"), hb.alloc_fp8_operand(M, K))
+    gy = torch.randn(M, N, generator=gen, device="cuda").bfloat16()
+    first = hb.fp8_weight_grad(gy, X, torch.empty(N, K, device="cuda"))
+    ref = gy.double().t() @ on_device((X,))
+    assert (first.double() - ref).norm() <= 2e-6 * ref.norm()      # 512 rows' truncated sums: 32 instructions of a step each at most
+    spoil = torch.empty(1 << 26, device="cuda")
+    for i in range(60):
+        if i % 3 == 0:
+            spoil.fill_(float("nan"))
+        GW = torch.full((N, K), float("nan"), device="cuda")
+        if i % 2:
+            GW.zero_()
+        assert torch.equal(hb.fp8_weight_grad(gy, X, GW, base=GW if i % 2 else None), first), i
+
+
 def test_weight_grad_rounds_other_scales_to_bf16(hb):
     """Scales that are no powers of two: X^ is the bf16 number next to code times scale."""
     X, x, _, _ = fu.held(normal(200, 300, 5), 1, "any")
