@@ -5,7 +5,6 @@
 // instruction's rows, rows of A its columns), scales them into fp32 registers and the warps' sums are added in warp order at the end.
 // Each lane reads 32 consecutive bytes of two rows of W (and of its row of A); which 32 elements of the group meet in which
 // instruction does not matter as long as both operands agree, so lane t of a quad takes bytes 32 t .. 32 t + 31.
-// One row, 4096 x 9216 (38 MB): 9.2 us, launch included; 1000 x 4096: 5.5 us.
 #include <cuda_bf16.h>
 #include "fp8_common.cuh"
 #include "kernels.h"
@@ -42,8 +41,9 @@ __device__ __forceinline__ uint4 codes16(const uint8_t* row, int64_t k, int64_t 
   return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
-// COLS: rows of A in eights.  WARPS, DEEP: warps per CTA and groups that a warp loads at a time; one row of A wants many warps (4096 x
-// 9216: 9.2 us with 16 warps and single groups, 10.1 with 8 and 2), two eights the registers for two groups (12.5 us; 17.6 with 16 and 1).
+// COLS: rows of A in eights.  WARPS, DEEP: warps per CTA and groups that a warp loads at a time.  Weights from memory (16 warps with
+// single groups / 8 with two / 8 with three): 1 x 4096 x 9216 15.6 / 13.5 / 12.4 us, 1 x 4096 x 4096 8.2 / 7.0 / 7.5, 1 x 1000 x 4096
+// (63 CTAs) 4.2 / 5.6 / 5.7, 16 with two 4.1; 16 rows of A, 4096 x 9216, from L2, 17.6 us with 16 and 1, 12.5 with 8 and 2.
 template <int COLS, int WARPS, int DEEP>
 __global__ void __launch_bounds__(WARPS * 32, WARPS == 16 ? 1 : 2)
 fp8_gemv_kernel(const Args g) {
@@ -131,8 +131,14 @@ cudaError_t launch_fp8_gemv(const Fp8View& A, const Fp8View& W, void* C, bool c_
   const Args g{A.codes, A.ld, A.scales, A.ld_s, W.codes, W.ld, W.scales, W.ld_s, C, ldc, c_bf16 ? 1 : 0, static_cast<int32_t>(A.rows), W.rows, A.K,
                (A.K + kGroup - 1) / kGroup};
   const dim3 grid(static_cast<unsigned>((W.rows + kRowsW - 1) / kRowsW));
+  int dev = 0, sms = 0;
+  const cudaError_t e = current_device(&dev, &sms);
+  if (e != cudaSuccess) return e;
   if (A.rows > 8) return launch_pdl(fp8_gemv_kernel<2, 8, 2>, grid, dim3(8 * 32), 0, stream, g);
-  return launch_pdl(fp8_gemv_kernel<1, 16, 1>, grid, dim3(16 * 32), 0, stream, g);
+  // one CTA per SM or fewer: more warps each; else two per SM, the longer rows with three groups in flight
+  if (static_cast<int>(grid.x) <= sms) return launch_pdl(fp8_gemv_kernel<1, 16, 2>, grid, dim3(16 * 32), 0, stream, g);
+  if (g.groups <= 32) return launch_pdl(fp8_gemv_kernel<1, 8, 2>, grid, dim3(8 * 32), 0, stream, g);
+  return launch_pdl(fp8_gemv_kernel<1, 8, 3>, grid, dim3(8 * 32), 0, stream, g);
 }
 
 }  // namespace hbmm
