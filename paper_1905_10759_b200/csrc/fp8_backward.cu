@@ -5,7 +5,8 @@
 //
 // Groups of a power of two up to 128 elements: the 128 elements that share a scale belong to 32 lanes of four (fp32) or 16 lanes
 // of eight (bf16): 16-byte gradients either way; group sums are shuffle trees inside them.
-// Other groups: a team of 2^t lanes per group, or a CTA per group of more than 1024, two walks over the group.
+// Other groups: four lanes, a warp, or (more than 1024 elements) a CTA per group, two walks over the group.
+// Measured: 8192 x 8192, groups of 32, bf16 (338 MB) 67 us, 5.0 TB/s; with five or six CTAs per SM 76 and 98.
 #include <cuda_bf16.h>
 #include "fp8_common.cuh"
 #include "kernels.h"

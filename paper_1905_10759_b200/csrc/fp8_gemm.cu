@@ -9,8 +9,9 @@
 //     accumulation in tensor memory, 256 columns;
 //   * otherwise each group's dot products go to one of three units of 128 columns, and the epilogue adds them, times the two scales,
 //     to fp32 registers.  The accumulation in tensor memory is left where it stands and taken first.
-// The second way is bound by the round trip from the MMA's completion to the epilogue and back (8192^3: 1.08 ms when every product
-// went that way); the first by the tensor cores' power (0.40 ms, 2.75 PFLOP/s; its MMAs alone 0.29 ms).
+// The second way costs 560 clk per 128 columns and group, MMA to epilogue and back (8192^3 with scales of any value 0.57 ms, 1.94
+// PFLOP/s; in seven units of 64 columns 1.17 ms); the first is bound by the tensor cores and their power (0.37 to 0.45 ms, 2.98 to 2.45
+// PFLOP/s, by how warm the part is; the MMAs alone 0.29 ms; tensor pipe 82 % active on 2048 x 8192 x 8192).
 //
 // C = A^ W^ (the input gradient; the contraction runs along the rows of W) reads the same W: its tiles arrive as 128 rows of the
 // contraction x 128 columns and enter the MMA as an MN-major operand.  Nothing is transposed in memory.

@@ -6,6 +6,7 @@
 // Each lane reads 32 consecutive bytes of two rows of W (and of its row of A); which 32 elements of the group meet in which
 // instruction does not matter as long as both operands agree, so lane t of a quad takes bytes 32 t .. 32 t + 31.
 #include <cuda_bf16.h>
+#include <type_traits>
 #include "fp8_common.cuh"
 #include "kernels.h"
 #include "pdl.cuh"
@@ -31,19 +32,22 @@ __device__ __forceinline__ void mma_e4m3(float (&d)[4], const uint32_t (&a)[4], 
   asm("mma.sync.aligned.m16n8k32.row.col.f32.e4m3.e4m3.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
       : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
-// 16 codes of a row from column k on; zeros past its end.
-__device__ __forceinline__ uint4 codes16(const uint8_t* row, int64_t k, int64_t K, bool in) {
-  if (in && k + 16 <= K) return load16(row + k);
+// 16 codes of a row from column k on; zeros past its end (WHOLE: it does not end before).
+template <bool WHOLE>
+__device__ __forceinline__ uint4 codes16(const uint8_t* row, int64_t k, int64_t K) {
+  if (WHOLE || k + 16 <= K) return load16(row + k);
   uint32_t w[4] = {0, 0, 0, 0};
-  if (in)
-    for (int e = 0; e < 16; e++)
-      if (k + e < K) w[e / 4] |= load1(row + k + e) << (8 * (e % 4));
+#pragma unroll
+  for (int e = 0; e < 16; e++)
+    if (k + e < K) w[e / 4] |= load1(row + k + e) << (8 * (e % 4));
   return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
-// COLS: rows of A in eights.  WARPS, DEEP: warps per CTA and groups that a warp loads at a time.  Weights from memory (16 warps with
-// single groups / 8 with two / 8 with three): 1 x 4096 x 9216 15.6 / 13.5 / 12.4 us, 1 x 4096 x 4096 8.2 / 7.0 / 7.5, 1 x 1000 x 4096
-// (63 CTAs) 4.2 / 5.6 / 5.7, 16 with two 4.1; 16 rows of A, 4096 x 9216, from L2, 17.6 us with 16 and 1, 12.5 with 8 and 2.
+// COLS: rows of A in eights.  WARPS, DEEP: warps per CTA and groups that a warp loads at a time.  Weights from memory, launch included:
+// 1 x 4096 x 9216 9.2 us, 1 x 8192 x 8192 14.9 (4.5 TB/s), 1 x 4096 x 4096 5.7, 1 x 1000 x 4096 3.6; 16 x 8192 x 8192 20.6.  How the
+// choices compared, before the loads of whole groups lost their checks (16 warps with single groups / 8 with two / 8 with three): 1 x
+// 4096 x 9216 15.6 / 13.5 / 12.4 us, 1 x 4096 x 4096 8.2 / 7.0 / 7.5, 1 x 1000 x 4096 (63 CTAs) 4.2 / 5.6 / 5.7, 16 with two 4.1; 16 rows
+// of A, 4096 x 9216, from L2, 17.6 us with 16 and 1, 12.5 with 8 and 2.  Groups kept in flight in a ring instead: 1 x 4096 x 9216 14.7.
 template <int COLS, int WARPS, int DEEP>
 __global__ void __launch_bounds__(WARPS * 32, WARPS == 16 ? 1 : 2)
 fp8_gemv_kernel(const Args g) {
@@ -51,29 +55,35 @@ fp8_gemv_kernel(const Args g) {
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, row = lane >> 2, quad = lane & 3;
   const int64_t n0 = static_cast<int64_t>(blockIdx.x) * kRowsW;
   pdl_wait();
-  const bool in0 = n0 + row < g.N, in1 = n0 + row + 8 < g.N;
-  const uint8_t *w0 = g.w + (in0 ? n0 + row : 0) * g.ld_w, *w1 = g.w + (in1 ? n0 + row + 8 : 0) * g.ld_w;
+  // a row past the end of an operand reads the first one: what comes of it is not stored
+  const uint8_t *w0 = g.w + (n0 + row < g.N ? n0 + row : 0) * g.ld_w, *w1 = g.w + (n0 + row + 8 < g.N ? n0 + row + 8 : 0) * g.ld_w;
   const float* ws = g.w_s + n0 / kGroup * g.ld_ws;       // 16 rows lie in one block of 128
+  const uint8_t* ar[COLS];
+  const float *s0[COLS], *s1[COLS];
+#pragma unroll
+  for (int t = 0; t < COLS; t++) {
+    const int m = 8 * t + row, c = 8 * t + 2 * quad;     // this lane's row of A as an operand, its two in the result
+    ar[t] = g.a + (m < g.M ? m : 0) * g.ld_a;
+    s0[t] = g.a_s + (c < g.M ? c : 0) * g.ld_as;
+    s1[t] = g.a_s + (c + 1 < g.M ? c + 1 : 0) * g.ld_as;
+  }
   float acc[COLS][4];
 #pragma unroll
   for (int t = 0; t < COLS; t++)
 #pragma unroll
     for (int e = 0; e < 4; e++) acc[t][e] = 0.0f;
   struct Loads { uint4 w[4], a[COLS][2]; float s[COLS][2], sw; };
-  const auto fetch = [&](int64_t gr, Loads& l) {
+  const auto fetch = [&](auto whole, int64_t gr, Loads& l) {
+    constexpr bool WHOLE = decltype(whole)::value;
     const int64_t k = gr * kGroup + quad * 32;
-    const bool live = gr < g.groups;
-    l.w[0] = codes16(w0, k, g.K, in0 && live); l.w[1] = codes16(w0, k + 16, g.K, in0 && live);
-    l.w[2] = codes16(w1, k, g.K, in1 && live); l.w[3] = codes16(w1, k + 16, g.K, in1 && live);
-    l.sw = live ? loadf(ws + gr) : 0.0f;
+    l.w[0] = codes16<WHOLE>(w0, k, g.K); l.w[1] = codes16<WHOLE>(w0, k + 16, g.K);
+    l.w[2] = codes16<WHOLE>(w1, k, g.K); l.w[3] = codes16<WHOLE>(w1, k + 16, g.K);
+    l.sw = loadf(ws + gr);
 #pragma unroll
     for (int t = 0; t < COLS; t++) {
-      const int m = 8 * t + row, c0 = 8 * t + 2 * quad;
-      const bool in = m < g.M && live;
-      const uint8_t* ar = g.a + (in ? m : 0) * g.ld_a;
-      l.a[t][0] = codes16(ar, k, g.K, in); l.a[t][1] = codes16(ar, k + 16, g.K, in);
-      l.s[t][0] = c0 < g.M && live ? loadf(g.a_s + c0 * g.ld_as + gr) : 0.0f;
-      l.s[t][1] = c0 + 1 < g.M && live ? loadf(g.a_s + (c0 + 1) * g.ld_as + gr) : 0.0f;
+      l.a[t][0] = codes16<WHOLE>(ar[t], k, g.K); l.a[t][1] = codes16<WHOLE>(ar[t], k + 16, g.K);
+      l.s[t][0] = loadf(s0[t] + gr);
+      l.s[t][1] = loadf(s1[t] + gr);
     }
   };
   const auto add = [&](const Loads& l) {
@@ -82,27 +92,38 @@ fp8_gemv_kernel(const Args g) {
 #pragma unroll
     for (int t = 0; t < COLS; t++) {
       const uint32_t b[8] = {l.a[t][0].x, l.a[t][0].y, l.a[t][0].z, l.a[t][0].w, l.a[t][1].x, l.a[t][1].y, l.a[t][1].z, l.a[t][1].w};
-      const float s0 = l.s[t][0] * l.sw, s1 = l.s[t][1] * l.sw;
+      const float f0 = l.s[t][0] * l.sw, f1 = l.s[t][1] * l.sw;
       float d[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
       for (int q = 0; q < 4; q++) {
         const uint32_t a[4] = {x[2 * q], y[2 * q], x[2 * q + 1], y[2 * q + 1]};
         mma_e4m3(d, a, b[2 * q], b[2 * q + 1]);
       }
-      acc[t][0] = fmaf(s0, d[0], acc[t][0]);
-      acc[t][1] = fmaf(s1, d[1], acc[t][1]);
-      acc[t][2] = fmaf(s0, d[2], acc[t][2]);
-      acc[t][3] = fmaf(s1, d[3], acc[t][3]);
+      acc[t][0] = fmaf(f0, d[0], acc[t][0]);
+      acc[t][1] = fmaf(f1, d[1], acc[t][1]);
+      acc[t][2] = fmaf(f0, d[2], acc[t][2]);
+      acc[t][3] = fmaf(f1, d[3], acc[t][3]);
     }
   };
-  for (int64_t gr = warp; gr < g.groups; gr += DEEP * WARPS) {
+  const int64_t full = g.K / kGroup;
+  int64_t gr = warp;
+  for (; gr + (DEEP - 1) * WARPS < full; gr += DEEP * WARPS) {
     Loads l[DEEP];
 #pragma unroll
-    for (int i = 0; i < DEEP; i++) fetch(gr + i * WARPS, l[i]);
+    for (int i = 0; i < DEEP; i++) fetch(std::true_type(), gr + i * WARPS, l[i]);
 #pragma unroll
-    for (int i = 0; i < DEEP; i++)
-      if (gr + i * WARPS < g.groups) add(l[i]);
+    for (int i = 0; i < DEEP; i++) add(l[i]);
   }
+  Loads rest[DEEP];                                      // fewer than DEEP groups of this warp, the last one perhaps short
+#pragma unroll
+  for (int i = 0; i < DEEP; i++) {
+    const int64_t at = gr + i * WARPS;
+    if (at < full) fetch(std::true_type(), at, rest[i]);
+    else if (at < g.groups) fetch(std::false_type(), at, rest[i]);
+  }
+#pragma unroll
+  for (int i = 0; i < DEEP; i++)
+    if (gr + i * WARPS < g.groups) add(rest[i]);
 #pragma unroll
   for (int t = 0; t < COLS; t++) {
     part[warp][row][8 * t + 2 * quad] = acc[t][0];

@@ -13,6 +13,9 @@
 //   warps 0-7   : epilogue (TMEM lanes 32 * (w % 4).., columns 128 * (w / 4)..)
 //   warp  8     : this CTA's copies;  warp 9 : TMEM allocation, MMA issue in the first CTA;  warp 10 : scales, up to 16 stages ahead
 //   warps 12-19 : converters
+// Measured: 8192 x 4096 x 4096 247 us, 1.11 PFLOP/s (tensor pipe half of the time active: the converters take 930 clk per stage, and
+// copies, conversion and MMA want 160 bytes of shared memory per clock at full rate, of 128); 256 x 4096 x 9216 45 us, 151 MB
+// written; 72 us with a base, 302 MB.
 // Few tiles: a cluster of two to four pairs shares each tile in equal parts of m (fp8_tile.cuh).
 #include <cuda_bf16.h>
 #include "fp8_tile.cuh"
