@@ -21,7 +21,7 @@ hbmm_status check_operand(const hbmm_fp8_operand* op, int32_t block_rows = 0) {
   if (!op || op->rows <= 0 || op->K <= 0) return HBMM_ERR_INVALID_ARG;
   if (op->block_rows != 1 && op->block_rows != kGroup) return HBMM_ERR_UNSUPPORTED;
   if (block_rows != 0 && op->block_rows != block_rows) return HBMM_ERR_UNSUPPORTED;
-  if (op->rows >= kMaxExtent || op->K >= kMaxExtent || op->ld_codes >= kMaxPitch) return HBMM_ERR_UNSUPPORTED;
+  if (op->rows >= kMaxExtent || op->K >= kMaxExtent || op->ld_codes >= kMaxPitch || op->ld_scales >= kMaxPitch) return HBMM_ERR_UNSUPPORTED;
   if (!op->codes || !op->scales || op->ld_codes < op->K || op->ld_scales < groups(op->K)) return HBMM_ERR_INVALID_ARG;
   if (!on16(op->codes) || !on16(op->scales) || op->ld_codes % 16 != 0 || op->ld_scales % 4 != 0) return HBMM_ERR_ALIGNMENT;
   return HBMM_OK;
@@ -32,7 +32,7 @@ Fp8View view_of(const hbmm_fp8_operand* op) { return {op->codes, op->scales, op-
 // A matrix whose rows start on 16-byte boundaries.
 hbmm_status check_rows(const void* p, int64_t cols, int64_t ld, int64_t size) {
   if (!p || ld < cols) return HBMM_ERR_INVALID_ARG;
-  if (ld * size >= kMaxPitch) return HBMM_ERR_UNSUPPORTED;
+  if (ld >= kMaxPitch / size) return HBMM_ERR_UNSUPPORTED;
   return on16(p) && ld * size % 16 == 0 ? HBMM_OK : HBMM_ERR_ALIGNMENT;
 }
 inline int64_t size_of(int32_t dtype) { return dtype == HBMM_BF16 ? 2 : 4; }

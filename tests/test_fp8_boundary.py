@@ -45,6 +45,7 @@ BAD_OPERANDS = [
     (dict(scales=None), hbmm.ERR_INVALID_ARG), (dict(ld_codes=240), hbmm.ERR_INVALID_ARG), (dict(ld_scales=1), hbmm.ERR_INVALID_ARG),
     (dict(ld_codes=264), hbmm.ERR_ALIGNMENT), (dict(ld_scales=6), hbmm.ERR_ALIGNMENT), (dict(codes=0x1008), hbmm.ERR_ALIGNMENT),
     (dict(scales=0x2004), hbmm.ERR_ALIGNMENT), (dict(block_rows=64), hbmm.ERR_UNSUPPORTED), (dict(rows=1 << 31), hbmm.ERR_UNSUPPORTED),
+    (dict(ld_codes=1 << 62), hbmm.ERR_UNSUPPORTED), (dict(ld_scales=1 << 62), hbmm.ERR_UNSUPPORTED),
 ]
 
 
@@ -83,7 +84,7 @@ def test_refusals():
         P(p), dt, N, ldg, by(X), P(b) if b else None, ldb, P(gw), ldw, None)
     assert wg(p=None) == wg(N=0) == wg(dt=3) == wg(ldg=56) == wg(gw=None) == wg(ldw=252) == wg(b=0x9000, ldb=128) == INV
     assert wg(b=0x8000, ldb=512) == INV                                                   # the gradient itself, another pitch
-    assert wg(dt=0) == wg(X=desc(rows=8, block_rows=128)) == UNS
+    assert wg(dt=0) == wg(X=desc(rows=8, block_rows=128)) == wg(ldg=1 << 62) == wg(ldw=1 << 61) == UNS
     assert wg(p=0x4008) == wg(ldg=68) == wg(gw=0x8008) == wg(ldw=258) == wg(b=0x9004, ldb=256) == wg(b=0x9000, ldb=257) == ALI
     bb = lambda X=x, p=0x4000, dt=0, ldg=256, beta=32, o=0x8000, ldo=256: lib.hbmm_fp8_binarize_backward(  # noqa: E731
         by(X), P(p), dt, ldg, beta, P(o), ldo, None)
