@@ -86,7 +86,8 @@ __device__ __forceinline__ void store_out4(const Out& o, int64_t m, int64_t n, f
 // their own rows and read the rows of a store instruction side by side.  Pieces of 16 bytes lie where neither conflicts.
 //   narrow: eight rows of 64 bytes at a time, 16 columns in fp32, 32 in bf16 (rounded on the way in);
 //   wide (fp32): 16 rows at a time, four rows of whole 128-byte lines per store, and the base, if any, half a step ahead of its use.
-// A block that lies inside the matrix goes without checks.
+//   (blocks that lie inside the matrix only: with a check per piece 256 x 4096 x 9216 outputs took 82 us instead of 45).
+// Elsewhere rows and columns that the matrix lacks are skipped piece by piece; a piece that it ends in goes element by element.
 constexpr int kStoreBytes = 2048;             // per warp
 __device__ __forceinline__ unsigned char* store_piece(unsigned char* stage, int row, int piece) { return stage + row * 64 + ((piece ^ (row >> 1 & 3)) << 4); }
 // The base's lines of a warp's 32 rows x 128 columns into L2, some time before store_tile reads them.
@@ -98,39 +99,18 @@ __device__ __forceinline__ void prefetch_base(const Out& o, int64_t m0, int64_t 
 }
 template <bool WIDE>
 __device__ __forceinline__ void store_tile(const Out& o, unsigned char* stage, const uint64_t (&acc)[kRun], int64_t m0, int64_t n0, int64_t n1, int lane) {
-  const int sub = lane / 4, piece = lane % 4;
-  const int64_t r0 = m0 + sub;
-  const bool inside = m0 + 32 <= o.M && n0 + kRun <= o.N && n1 + kRun <= o.N;
-  if (!WIDE && inside && o.bf16) {                      // 32 columns at a time, rounded on the way in
-    __nv_bfloat16* out = static_cast<__nv_bfloat16*>(o.c) + r0 * o.ldc + n0 + piece * 8;
-#pragma unroll
-    for (int c = 0; c < 4; c++) {
-      __syncwarp();
-#pragma unroll
-      for (int p = 0; p < 4; p++) {
-        uint32_t w[4];
-#pragma unroll
-        for (int e = 0; e < 4; e++) {
-          float lo, hi;
-          unpack2(acc[c * 16 + p * 4 + e], lo, hi);
-          w[e] = bf16x2(lo, hi);
-        }
-        *reinterpret_cast<uint4*>(store_piece(stage, lane, p)) = make_uint4(w[0], w[1], w[2], w[3]);
-      }
-      __syncwarp();
-#pragma unroll
-      for (int i = 0; i < 4; i++)
-        *reinterpret_cast<uint4*>(out + i * 8 * o.ldc) = *reinterpret_cast<const uint4*>(store_piece(stage, i * 8 + sub, piece));
-      out += c == 1 ? n1 - n0 - 32 : 32;
-    }
-    return;
-  }
-  if (WIDE && inside && !o.bf16) {
-    const int sub8 = lane / 8, piece8 = lane % 8;
-    const int64_t r8 = m0 + sub8;
-    float* out = static_cast<float*>(o.c) + r8 * o.ldc + n0 + piece8 * 4;
+  if (m0 >= o.M) return;
+  const int rows = o.M - m0 < 32 ? static_cast<int>(o.M - m0) : 32;
+  const auto left = [&](int64_t n) { return o.N - n < 64 ? static_cast<int>(o.N - n) : 64; };       // columns from n on, 0 or less: none
+  const auto words = [&](int j) {                       // four consecutive columns of this lane's row, raw
+    return make_uint4(static_cast<uint32_t>(acc[j]), static_cast<uint32_t>(acc[j] >> 32), static_cast<uint32_t>(acc[j + 1]), static_cast<uint32_t>(acc[j + 1] >> 32));
+  };
+  if (WIDE && rows == 32 && n0 + kRun <= o.N && n1 + kRun <= o.N) {
+    const int sub = lane / 8, piece = lane % 8;
+    const int64_t r0 = m0 + sub;
+    float* out = static_cast<float*>(o.c) + r0 * o.ldc + n0 + piece * 4;
     const bool base = o.base != nullptr;
-    const float* from = base ? o.base + r8 * o.ld_base + n0 + piece8 * 4 : nullptr;
+    const float* from = base ? o.base + r0 * o.ld_base + n0 + piece * 4 : nullptr;
     uint4 ahead[4];
     if (base) {
 #pragma unroll
@@ -144,15 +124,12 @@ __device__ __forceinline__ void store_tile(const Out& o, unsigned char* stage, c
         __syncwarp();
         if (lane / 16 == hf) {
 #pragma unroll
-          for (int p = 0; p < 8; p++)
-            *reinterpret_cast<uint4*>(swz(stage, lane % 16, p)) =
-                make_uint4(static_cast<uint32_t>(acc[c * 16 + 2 * p]), static_cast<uint32_t>(acc[c * 16 + 2 * p] >> 32),
-                           static_cast<uint32_t>(acc[c * 16 + 2 * p + 1]), static_cast<uint32_t>(acc[c * 16 + 2 * p + 1] >> 32));
+          for (int p = 0; p < 8; p++) *reinterpret_cast<uint4*>(swz(stage, lane % 16, p)) = words(c * 16 + 2 * p);
         }
         __syncwarp();
 #pragma unroll
         for (int i = 0; i < 4; i++) {
-          float4 v = *reinterpret_cast<const float4*>(swz(stage, i * 4 + sub8, piece8));
+          float4 v = *reinterpret_cast<const float4*>(swz(stage, i * 4 + sub, piece));
           if (base) {
             v.x += __uint_as_float(ahead[i].x); v.y += __uint_as_float(ahead[i].y);
             v.z += __uint_as_float(ahead[i].z); v.w += __uint_as_float(ahead[i].w);
@@ -169,26 +146,62 @@ __device__ __forceinline__ void store_tile(const Out& o, unsigned char* stage, c
     }
     return;
   }
-  const bool plain = inside && !o.bf16;
+  const int sub = lane / 4, piece = lane % 4;
+  const int64_t r0 = m0 + sub;
+  if (!WIDE && o.bf16) {                                // 32 columns at a time, rounded on the way in
+    __nv_bfloat16* out = static_cast<__nv_bfloat16*>(o.c) + r0 * o.ldc + n0 + piece * 8;
+#pragma unroll
+    for (int c = 0; c < 4; c++) {
+      const int64_t n = (c < 2 ? n0 : n1) + c % 2 * 32;
+      __syncwarp();
+#pragma unroll
+      for (int p = 0; p < 4; p++) {
+        uint32_t w[4];
+#pragma unroll
+        for (int e = 0; e < 4; e++) {
+          float lo, hi;
+          unpack2(acc[c * 16 + p * 4 + e], lo, hi);
+          w[e] = bf16x2(lo, hi);
+        }
+        *reinterpret_cast<uint4*>(store_piece(stage, lane, p)) = make_uint4(w[0], w[1], w[2], w[3]);
+      }
+      __syncwarp();
+      const int cols = left(n + piece * 8);
+#pragma unroll
+      for (int i = 0; i < 4; i++) {
+        if (i * 8 + sub >= rows) continue;
+        const uint4 v = *reinterpret_cast<const uint4*>(store_piece(stage, i * 8 + sub, piece));
+        __nv_bfloat16* to = out + i * 8 * o.ldc;
+        if (cols >= 8) {
+          *reinterpret_cast<uint4*>(to) = v;
+        } else {
+          const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+          for (int e = 0; e < 7; e++)
+            if (e < cols) reinterpret_cast<unsigned short*>(to)[e] = static_cast<unsigned short>(w[e / 2] >> (16 * (e % 2)));
+        }
+      }
+      out += c == 1 ? n1 - n0 - 32 : 32;
+    }
+    return;
+  }
   float* out = static_cast<float*>(o.c) + r0 * o.ldc + n0 + piece * 4;
 #pragma unroll
   for (int c = 0; c < 8; c++) {
+    const int64_t n = (c < 4 ? n0 : n1) + c % 4 * 16;
     __syncwarp();                                       // the columns before have been read
 #pragma unroll
-    for (int p = 0; p < 4; p++)
-      *reinterpret_cast<uint4*>(store_piece(stage, lane, p)) =
-          make_uint4(static_cast<uint32_t>(acc[c * 8 + 2 * p]), static_cast<uint32_t>(acc[c * 8 + 2 * p] >> 32),
-                     static_cast<uint32_t>(acc[c * 8 + 2 * p + 1]), static_cast<uint32_t>(acc[c * 8 + 2 * p + 1] >> 32));
+    for (int p = 0; p < 4; p++) *reinterpret_cast<uint4*>(store_piece(stage, lane, p)) = words(c * 8 + 2 * p);
     __syncwarp();
-    if (!WIDE && plain) {
+    const int cols = left(n + piece * 4);
 #pragma unroll
-      for (int i = 0; i < 4; i++) *reinterpret_cast<float4*>(out + i * 8 * o.ldc) = *reinterpret_cast<const float4*>(store_piece(stage, i * 8 + sub, piece));
-      out += c == 3 ? n1 - n0 - kRun + 16 : 16;
-    } else {
-#pragma unroll
-      for (int i = 0; i < 4; i++)
-        store_out4(o, r0 + i * 8, (c < 4 ? n0 : n1) + (c % 4) * 16 + piece * 4, *reinterpret_cast<const float4*>(store_piece(stage, i * 8 + sub, piece)));
+    for (int i = 0; i < 4; i++) {
+      if (i * 8 + sub >= rows) continue;
+      const float4 v = *reinterpret_cast<const float4*>(store_piece(stage, i * 8 + sub, piece));
+      if (cols >= 4 && !(WIDE && o.base)) *reinterpret_cast<float4*>(out + i * 8 * o.ldc) = v;
+      else if (cols > 0) store_out4(o, r0 + i * 8, n + piece * 4, v);
     }
+    out += c == 3 ? n1 - n0 - kRun + 16 : 16;
   }
 }
 
