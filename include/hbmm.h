@@ -432,8 +432,9 @@ hbmm_status hbmm_fp8_quantize(const void *x, int32_t x_dtype, int64_t rows, int6
 
 /*
  * C[m,n] = sum_g sA[m,g] sW[n/128,g] sum_{k in group g} A[m,k] W[n,k]: the forward product of a layer, for one row of A
- * (a single token) up to long batches.  A: M x K, block_rows 1.  W: N x K, block_rows 128.  Any scales, their product
- * finite.  A dot product over a group is formed by the tensor cores, groups are summed in fp32.
+ * (a single token) up to long batches.  A: M x K, block_rows 1.  W: N x K, block_rows 128.  Any scales, the
+ * products of two that meet normal fp32 numbers (a smaller product may count as zero, a larger one as infinite).  A dot
+ * product over a group is formed by the tensor cores, groups are summed in fp32.
  * C: device [M, ldc] of c_dtype (fp32, or bf16 rounded to nearest even), ldc >= N, rows on 16-byte boundaries; fully
  * overwritten in columns < N.  A NaN code makes its row (of A) or its column (of W) of C NaN and nothing else.
  * C may not overlap the operands.  Errors: INVALID_ARG, UNSUPPORTED (block_rows, sizes), ALIGNMENT, CUDA.
