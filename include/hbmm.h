@@ -464,7 +464,8 @@ hbmm_status hbmm_fp8_weight_grad(const void *gy, int32_t gy_dtype, int64_t N, in
 
 /*
  * hbmm_binarize_backward (Eq. 6) from the 8-bit copy of x: X^ = codes times scales stands for x in the group means and in
- * [|x| <= 1], Sign(x) is the code's sign bit (of every element that hbmm_fp8_quantize wrote the sign of x itself).
+ * [|x| <= 1], Sign(x) is the code's sign bit (of every element that hbmm_fp8_quantize wrote the sign of x itself), whatever
+ * the scale's own sign.  Group sums in fp32.
  * X: block_rows 1.  gy, gx: device [rows, ld*] of dtype (both), ld* >= K, aligned to their element.  beta >= 1, any value.
  * gx may not overlap X or gy.  Errors: INVALID_ARG, UNSUPPORTED (block_rows, sizes), ALIGNMENT, CUDA.
  */
