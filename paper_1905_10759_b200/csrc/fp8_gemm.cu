@@ -22,8 +22,9 @@
 //   warp  8     : one thread issues this CTA's copies;  warp 9 : TMEM allocation, and in the first CTA the MMA-issuing thread
 //   warp  10    : copies each step's scales to shared memory, up to eight steps ahead (11 hands over registers)
 //   warps 12-15 : scouts: look the scales over and write their exponents to tensor memory
-// What both CTAs have to know (their scales' kind) goes as asynchronous stores that complete on the barrier the readers wait at; the
-// arrivals across the pair release nothing but reads.  (Store and releasing arrival: 2600 clk beside the copies, 0.53 ms.)
+// What one CTA writes and the other depends on (the factors, which the first CTA's MMAs take from both tensor memories, and the kind
+// of the scales) is announced by asynchronous stores that complete on the barrier the readers wait at, a release at cluster scope;
+// the arrivals across the pair release nothing but reads.  (Store and releasing arrival: 2600 clk beside the copies, 0.53 ms.)
 // Products of few tiles: a cluster of two to four pairs shares each tile in equal parts of K (fp8_tile.cuh).
 #include <cuda_bf16.h>
 #include "fp8_tile.cuh"
@@ -52,7 +53,8 @@ constexpr int kUnit = 128, kUnits = 3, kTurns = 2 * kUnits, kFactorCols = 384, k
 constexpr int OFF_A = 0, OFF_B = STAGES * kTile, OFF_OUT = STAGES * STAGE, OFF_SCALES = OFF_OUT + kEpilogueWarps * kStoreBytes;
 constexpr int OFF_BAR = OFF_SCALES + kSlots * kSlotBytes;
 constexpr int kBars = 2 * STAGES + 2 * kTurns + 2 + 3 * kSlots + 1;
-constexpr int OFF_FLAGS = OFF_BAR + kBars * 8, kBytes = OFF_FLAGS + kSlots * 8 + 16;
+constexpr int kScouts = 4, kFlags = 2 * kScouts;                             // words of a slot: one from each scout of both CTAs
+constexpr int OFF_FLAGS = OFF_BAR + kBars * 8, kBytes = OFF_FLAGS + kSlots * kFlags * 4 + 16;
 static_assert(kBytes <= 227 * 1024 && TM * TN * 4 <= STAGES * STAGE && kFactorCols + kSlots * kFactorSlot <= 512, "shared and tensor memory");
 
 struct Args {
@@ -88,8 +90,8 @@ fp8_gemm_kernel(const Args g, const __grid_constant__ CUtensorMap a_map, const _
   uint64_t* sfull = scales + kSlots;           // its factors are in both CTAs' tensor memory, and how it is summed is known
   uint64_t* sempty = sfull + kSlots;           // its slot is free in both CTAs
   uint64_t* drained = sempty + kSlots;
-  uint32_t* flags = reinterpret_cast<uint32_t*>(smem + OFF_FLAGS);             // [kSlots][CTA of the pair]: the scales are factors
-  uint32_t* tmem_base_ptr = flags + kSlots * 2;
+  uint32_t* flags = reinterpret_cast<uint32_t*>(smem + OFF_FLAGS);             // [kSlots][CTA of the pair][scout]: the scales are factors
+  uint32_t* tmem_base_ptr = flags + kSlots * kFlags;
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_base_ptr + 1);
 
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -113,7 +115,7 @@ fp8_gemm_kernel(const Args g, const __grid_constant__ CUtensorMap a_map, const _
     mbar_init(xempty, 2 * kEpilogueWarps);
     for (int f = 0; f < kSlots; f++) {
       mbar_init(&scales[f], 32);                            // the scale loader's lanes
-      mbar_init(&sfull[f], 8);                              // scout warps of both CTAs
+      mbar_init(&sfull[f], kScouts);                        // this CTA's scouts; the words of both CTAs' complete the bytes
       mbar_init(&sempty[f], 2 * kEpilogueWarps + 1);        // epilogue warps of both CTAs, MMA commit
     }
     mbar_init(drained, 1);
@@ -131,9 +133,9 @@ fp8_gemm_kernel(const Args g, const __grid_constant__ CUtensorMap a_map, const _
   tc_fence_after();
   const uint32_t tmem_base = *tmem_base_ptr;
   const Waiter wait{g_spin_limit, abort_flag};
-  const auto are_factors = [&](uint32_t f) {           // behind sfull
-    const volatile uint32_t* v = flags + f * 2;
-    return (v[0] & v[1]) != 0;
+  const auto are_factors = [&](uint32_t f) {           // behind sfull; a CTA's scouts have looked at the same scales
+    const volatile uint32_t* v = flags + f * kFlags;
+    return (v[0] & v[kScouts]) != 0;
   };
 
   if (warp >= kScoutWarp) reg_dec<kRegsScout>();
@@ -245,7 +247,7 @@ fp8_gemm_kernel(const Args g, const __grid_constant__ CUtensorMap a_map, const _
           open = 0;
         };
         for (int kb0 = g0; kb0 < g1 && ok; kb0 += kStep) {
-          if (!wait(smem_u32(&sfull[f]), f_par, 7)) { ok = false; break; }
+          if (!wait.cluster(smem_u32(&sfull[f]), f_par, 7)) { ok = false; break; }
           tc_fence_after();
           const int n = g1 - kb0 < kStep ? g1 - kb0 : kStep;
           if (are_factors(f)) {
@@ -349,15 +351,12 @@ fp8_gemm_kernel(const Args g, const __grid_constant__ CUtensorMap a_map, const _
         tc_fence_before();
         __syncwarp();
         if (lane == 0) {
-          const uint32_t bar = smem_u32(&sfull[f]);
-          if (quarter == 0) {                              // both CTAs' verdicts to both CTAs
-            for (uint32_t c = 0; c < 2; c++)
-              st_async_u32(mapa_rank(smem_u32(flags + f * 2 + half), lead + c), good ? 1u : 0u, mapa_rank(bar, lead + c));
-            mbar_arrive_expect_tx(&sfull[f], 8);
-          } else {
-            mbar_arrive(&sfull[f]);
-          }
-          mbar_arrive_cluster_read(mapa_rank(bar, rank ^ 1u));
+          // the verdict to both CTAs, and with it that this scout's factors are written
+          for (uint32_t c = 0; c < 2; c++)
+            st_async_u32(mapa_rank(smem_u32(flags + f * kFlags + half * kScouts + quarter), lead + c), good ? 1u : 0u,
+                         mapa_rank(smem_u32(&sfull[f]), lead + c));
+          if (quarter == 0) mbar_arrive_expect_tx(&sfull[f], kFlags * 4);
+          else mbar_arrive(&sfull[f]);
         }
         __syncwarp();
         if (++f == kSlots) { f = 0; f_par ^= 1; }
@@ -396,7 +395,7 @@ fp8_gemm_kernel(const Args g, const __grid_constant__ CUtensorMap a_map, const _
       };
       // `open` counts as the MMA issuer's does; a full accumulator is taken at the next step or at the tile's end
       for (int kb0 = g0; kb0 < g1 && ok; kb0 += kStep) {
-        if (!wait(smem_u32(&sfull[f]), f_par, 6)) { ok = false; break; }
+        if (!wait.cluster(smem_u32(&sfull[f]), f_par, 6)) { ok = false; break; }
         const bool factors = are_factors(f);
         const int n = g1 - kb0 < kStep ? g1 - kb0 : kStep;
         if (open != 0 && (!factors || open == kChunk) && !take_accumulator()) { ok = false; break; }

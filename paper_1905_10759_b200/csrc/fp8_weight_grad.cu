@@ -12,7 +12,10 @@
 // against 32 elements per converting thread.  The two accumulators of 256 columns let a tile's epilogue run beside the next one's MMAs.
 //   warps 0-7   : epilogue (TMEM lanes 32 * (w % 4).., columns 128 * (w / 4)..)
 //   warp  8     : this CTA's copies;  warp 9 : TMEM allocation, MMA issue in the first CTA;  warp 10 : scales, up to 16 stages ahead
-//   warps 12-19 : converters
+//   warps 12-19 : converters;  warp 11, in the second CTA : tells the first that a stage is converted
+// The first CTA's MMAs read what the second one's converters wrote.  These arrive at a barrier of their own CTA; a thread that waits
+// there announces the stage by an asynchronous store, whose completion is a release at cluster scope and holds nobody up.  (8192 x
+// 4096 x 4096: 250 us; with that store from the converters 280, with releasing arrivals 443, from the waiting thread 361 to 465.)
 // Measured: 8192 x 4096 x 4096 247 us, 1.11 PFLOP/s (tensor pipe half of the time active: the converters take 930 clk per stage, and
 // copies, conversion and MMA want 160 bytes of shared memory per clock at full rate, of 128); 256 x 4096 x 9216 45 us, 151 MB
 // written; 72 us with a base, 302 MB.
@@ -29,14 +32,14 @@ namespace {
 using namespace fp8;
 
 constexpr int TN = 256, ROWS = 64;             // columns of a pair's tile; rows of the contraction per stage
-constexpr int kThreads = 20 * 32, kEpilogueWarps = 8, kLoaderWarp = 8, kMmaWarp = 9, kScaleWarp = 10, kConvertWarp = 12, kConvertWarps = 8;
+constexpr int kThreads = 20 * 32, kEpilogueWarps = 8, kLoaderWarp = 8, kMmaWarp = 9, kScaleWarp = 10, kRelayWarp = 11, kConvertWarp = 12, kConvertWarps = 8;
 constexpr int kOperand = 128 * ROWS * 2, kCodes = 128 * ROWS, STAGES = 5;          // bytes per stage of gy and of converted X; of codes
 constexpr int kChunkBytes = ROWS * 128;        // 64 columns of an operand: 128 bytes per row
 constexpr int kSlots = 16;                     // stages of scales
 constexpr int OFF_A = 0, OFF_B = STAGES * kOperand, OFF_CODES = 2 * STAGES * kOperand, OFF_OUT = OFF_CODES + STAGES * kCodes;
 constexpr int OFF_SCALES = OFF_OUT + kEpilogueWarps * kStoreBytes, OFF_BAR = OFF_SCALES + kSlots * ROWS * 4;
-constexpr int kBars = 5 * STAGES + 2 * kSlots + 5;
-constexpr int kBytes = OFF_BAR + kBars * 8 + 16;
+constexpr int kBars = 6 * STAGES + 2 * kSlots + 5;
+constexpr int kBytes = OFF_BAR + kBars * 8 + 16 + STAGES * 4;
 // An accumulator in tensor memory takes 512 rows, the epilogue adds it to fp32 registers: the tensor cores' additions truncate, always
 // towards zero, and with 8192 rows of sizes from 2^-8 to 2^8 in one accumulator the result was 9e-6 off.
 constexpr int kChunkStages = 512 / ROWS;
@@ -58,7 +61,8 @@ fp8_weight_grad_kernel(const Args g, const __grid_constant__ CUtensorMap gy_map,
   // a half would wait for the same parity at every visit, and pass when the other half's codes have not come yet)
   uint64_t* cfull = afull + STAGES;
   uint64_t* bfull = cfull + 2 * STAGES;        // first CTA: converted, in both CTAs
-  uint64_t* empty = bfull + STAGES;
+  uint64_t* bdone = bfull + STAGES;            // second CTA: converted here
+  uint64_t* empty = bdone + STAGES;
   uint64_t* sfull = empty + STAGES;            // scales of a stage
   uint64_t* sempty = sfull + kSlots;
   uint64_t* tfull = sempty + kSlots;
@@ -66,6 +70,7 @@ fp8_weight_grad_kernel(const Args g, const __grid_constant__ CUtensorMap gy_map,
   uint64_t* drained = tempty + 2;
   uint32_t* tmem_base_ptr = reinterpret_cast<uint32_t*>(drained + 1);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_base_ptr + 1);
+  uint32_t* told = tmem_base_ptr + 2;          // first CTA, [STAGES]: where the second one's announcements land
 
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const uint32_t rank = cluster_ctarank(), lead = rank & ~1u, half = rank & 1u;
@@ -80,7 +85,8 @@ fp8_weight_grad_kernel(const Args g, const __grid_constant__ CUtensorMap gy_map,
       mbar_init(&afull[s], 1);
       mbar_init(&cfull[s], 1);
       mbar_init(&cfull[STAGES + s], 1);
-      mbar_init(&bfull[s], kConvertWarps);                  // one half of the converters of each CTA
+      mbar_init(&bfull[s], kConvertWarps / 2 + 1);          // one half of this CTA's converters; its loader's expect_tx for the other CTA's word
+      mbar_init(&bdone[s], kConvertWarps / 2);
       mbar_init(&empty[s], 1);
     }
     for (int s = 0; s < kSlots; s++) { mbar_init(&sfull[s], 32); mbar_init(&sempty[s], kConvertWarps / 2); }
@@ -118,7 +124,10 @@ fp8_weight_grad_kernel(const Args g, const __grid_constant__ CUtensorMap gy_map,
         const int32_t n_at = static_cast<int32_t>(tm * 2 * TM + half * TM), k_at = static_cast<int32_t>(tn * TN + half * (TN / 2));
         for (int st = s0; st < s1; st++) {
           if (!wait(smem_u32(&empty[s]), par, 1)) { ok = false; break; }
-          if (half == 0) mbar_arrive_expect_tx(&afull[s], 2 * kOperand);
+          if (half == 0) {
+            mbar_arrive_expect_tx(&afull[s], 2 * kOperand);
+            mbar_arrive_expect_tx(&bfull[s], 4);
+          }
           mbar_arrive_expect_tx(&cfull[c], kCodes);
           tma_load_2d(smem + OFF_CODES + s * kCodes, &x_map, k_at, st * ROWS, &cfull[c]);
           if (++c == 2 * STAGES) c = 0;
@@ -165,12 +174,26 @@ fp8_weight_grad_kernel(const Args g, const __grid_constant__ CUtensorMap gy_map,
     }
     cp_async_wait_all();                                 // also after an abort
     __syncwarp();
+  } else if (warp == kRelayWarp) {
+    // =========================== announcements (second CTA) ===========================
+    if (half != 0 && elect_one()) {
+      const uint32_t bfull0 = mapa_rank(smem_u32(bfull), lead), told0 = mapa_rank(smem_u32(told), lead);
+      uint32_t s = 0, par = 0;
+      bool ok = true;
+      for (int64_t tile = walker; tile < n_tiles && ok; tile += walkers)
+        for (int st = s0; st < s1; st++) {
+          if (!wait(smem_u32(&bdone[s]), par, 7)) { ok = false; break; }
+          st_async_u32(told0 + s * 4, 1u, bfull0 + s * 8);
+          if (++s == STAGES) { s = 0; par ^= 1; }
+        }
+    }
+    __syncwarp();
   } else if (warp >= kConvertWarp) {
     // =========================== converters (both CTAs) ===========================
     // Four warps per stage, the other four on the next one: a warp's waits and its fence come once per four items of work.
     const int me = tid - kConvertWarp * 32 & 127;
     const uint32_t mine = (warp - kConvertWarp) / 4;
-    const uint32_t bfull0 = mapa_rank(smem_u32(bfull), lead);
+    uint64_t* converted = half == 0 ? bfull : bdone;
     const int q = me & 7;                                // 16 codes from column 16 q, rows me / 8 + 16 i
     uint32_t s = 0, c = 0, c_par = 0, f = 0, f_par = 0, turn = 0;
     bool ok = true;
@@ -204,7 +227,7 @@ fp8_weight_grad_kernel(const Args g, const __grid_constant__ CUtensorMap gy_map,
           fence_async_proxy();                           // the stores are the tensor core's to read
           __syncwarp();
           if (lane == 0) {
-            mbar_arrive_cluster_read(bfull0 + s * 8);
+            mbar_arrive(&converted[s]);
             mbar_arrive(&sempty[f]);
           }
         }
@@ -231,7 +254,7 @@ fp8_weight_grad_kernel(const Args g, const __grid_constant__ CUtensorMap gy_map,
           const uint32_t buf = acc & 1;
           if (acc >= 2 && !wait(tempty_a + buf * 8, ((acc >> 1) & 1) ^ 1, 3)) { ok = false; break; }
           for (int st = c0; st < c1; st++) {
-            if (!wait(afull_a + s * 8, par, 2) || !wait(bfull_a + s * 8, par, 2)) { ok = false; break; }
+            if (!wait(afull_a + s * 8, par, 2) || !wait.cluster(bfull_a + s * 8, par, 2)) { ok = false; break; }
             tc_fence_after();
             const uint32_t a_lo = da_lo + s * (kOperand >> 4), b_lo = db_lo + s * (kOperand >> 4);
 #pragma unroll

@@ -38,6 +38,14 @@ __device__ __forceinline__ bool mbar_try_wait_a(uint32_t bar, uint32_t parity) {
                : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
   return ok != 0;
 }
+// The same with an acquire at cluster scope (the one above acquires within the CTA): what another CTA of the cluster released on
+// the barrier is seen.
+__device__ __forceinline__ bool mbar_try_wait_cluster_a(uint32_t bar, uint32_t parity) {
+  uint32_t ok;
+  asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+               : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+  return ok != 0;
+}
 __device__ __forceinline__ void umma_commit_a(uint32_t bar) {
   asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
 }
@@ -261,8 +269,10 @@ __device__ __forceinline__ uint32_t mapa_rank(uint32_t addr, uint32_t rank) {
 __device__ __forceinline__ void mbar_arrive_cluster(uint32_t cluster_addr) {
   asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
 }
-// A word to the shared memory of a CTA of the cluster; its four bytes complete on a barrier of that CTA, so that whoever waits there
-// sees it and the writer waits for nothing (a store and an arrival that releases it take 2600 clk beside a stream of tensor copies).
+// A word to the shared memory of a CTA of the cluster; its four bytes complete on a barrier of that CTA.  The completion is a release
+// at cluster scope, so that whoever waits there (with an acquire at cluster scope) sees the word and what the writer did before it,
+// and the writer waits for nothing: this is how something written is announced across a pair.  (An arrival with .release.cluster, or
+// a fence of that scope before any other, holds its thread 1500 to 2600 clk beside a stream of tensor copies.)
 __device__ __forceinline__ void st_async_u32(uint32_t cluster_addr, uint32_t v, uint32_t cluster_bar) {
   asm volatile("st.async.weak.shared::cluster.mbarrier::complete_tx::bytes.u32 [%0], %1, [%2];" ::"r"(cluster_addr), "r"(v), "r"(cluster_bar) : "memory");
 }
@@ -271,19 +281,24 @@ __device__ __forceinline__ void st_async_u32(uint32_t cluster_addr, uint32_t v, 
 struct Waiter {
   uint32_t limit;
   volatile int* abort_flag;
-  __device__ __forceinline__ bool operator()(uint32_t bar, uint32_t parity, int code) const {
-    if (mbar_try_wait_a(bar, parity)) return true;
+  template <bool CLUSTER>
+  __device__ __forceinline__ bool wait(uint32_t bar, uint32_t parity, int code) const {
+    if (CLUSTER ? mbar_try_wait_cluster_a(bar, parity) : mbar_try_wait_a(bar, parity)) return true;
     for (uint32_t it = 0; it < limit; it++) {
-      if (mbar_try_wait_a(bar, parity)) return true;
+      if (CLUSTER ? mbar_try_wait_cluster_a(bar, parity) : mbar_try_wait_a(bar, parity)) return true;
       if (*abort_flag) return false;
     }
     atomicCAS(&g_error_word, 0, code);
     *abort_flag = 1;
     return false;
   }
+  __device__ __forceinline__ bool operator()(uint32_t bar, uint32_t parity, int code) const { return wait<false>(bar, parity, code); }
+  // for what another CTA wrote and announced by st_async_u32
+  __device__ __forceinline__ bool cluster(uint32_t bar, uint32_t parity, int code) const { return wait<true>(bar, parity, code); }
 };
-// The same for an arrival that only says that this thread has read (tensor memory, shared memory): nothing that it wrote has to be
-// seen by the other CTA.  The release above waits for the thread's stores, 2600 clk behind a tile's.
+// An arrival across the cluster that only says that this thread has read (tensor memory, shared memory): nothing that it wrote has
+// to be seen by the other CTA (its release is within the CTA).  mbar_arrive_cluster waits for the thread's stores, 2600 clk behind a
+// tile's.
 __device__ __forceinline__ void mbar_arrive_cluster_read(uint32_t cluster_addr) {
   asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
 }
