@@ -46,9 +46,14 @@ constexpr int STAGE = 2 * kTile, STAGES = 6;
 constexpr int kStep = 4, kSlots = 8, kScalesA = 128 * kStep * 4, kSlotBytes = kScalesA + 128;
 // Tensor memory: three units of 128 columns for partial sums (a whole accumulator takes the first two), then the factors of each
 // slot, 16 columns (4 of A, 8 of W).
-// A whole accumulator takes 16 steps (8192 elements) at most: the tensor cores' fp32 sums truncate, and the relative error of a result
-// grows with their number (256 x 256 outputs of K = 4096 / 8192: 7e-8 / 1.2e-7, 6e-8 / 7.5e-8 with a sum per group).
-constexpr int kChunk = 16;
+// A whole accumulator takes a run of kChunk steps, then the epilogue adds it to fp32 registers.  An instruction cuts its 32 products and
+// the sum so far below 2^-25 of the largest of them and truncates what they add up to (always towards zero), so the error of a run
+// grows with its length where nothing cancels.  Positive operands, groups of sizes from 2^-12 to 2^12, K = 16384, relative to the
+// norm: 1.3e-5 with runs of 8192 elements, 5.4e-6 with 4096, 2.9e-6 with 2048, 1.5e-6 with 1024, 8e-7 with 512; random signs and
+// one size, K = 8192: 1.2e-7, 7.6e-8 with 1024.  Taking an accumulator holds the MMAs up: 8192^3 381 us with runs of 8192, 390 with
+// 4096, 408 with 2048, 444 with 1024; 8192 x 4096 x 4096 99, 99, 103, 119.  An fp32 result gets 2048, as below that the time grows
+// faster than the error falls; a bf16 result, whose own rounding is up to 3.9e-3, gets 8192.
+constexpr int kChunkF32 = 4, kChunkBF16 = 16;
 constexpr int kUnit = 128, kUnits = 3, kTurns = 2 * kUnits, kFactorCols = 384, kFactorSlot = 16;
 constexpr int OFF_A = 0, OFF_B = STAGES * kTile, OFF_OUT = STAGES * STAGE, OFF_SCALES = OFF_OUT + kEpilogueWarps * kStoreBytes;
 constexpr int OFF_BAR = OFF_SCALES + kSlots * kSlotBytes;
@@ -100,7 +105,7 @@ fp8_gemm_kernel(const Args g, const __grid_constant__ CUtensorMap a_map, const _
   const int part = static_cast<int>(rank >> 1);
   // the pair's walk: tiles of its own, or one tile's groups [g0, g1) of `parts`
   const int64_t walker = blockIdx.x / (2 * g.parts), walkers = gridDim.x / (2 * g.parts);
-  const int steps = (g.groups + kStep - 1) / kStep;
+  const int steps = (g.groups + kStep - 1) / kStep, chunk = g.out.bf16 ? kChunkBF16 : kChunkF32;
   const int g0 = static_cast<int>(static_cast<int64_t>(part) * steps / g.parts) * kStep;
   const int g_end = static_cast<int>(static_cast<int64_t>(part + 1) * steps / g.parts) * kStep, g1 = g_end < g.groups ? g_end : g.groups;
 
@@ -266,7 +271,7 @@ fp8_gemm_kernel(const Args g, const __grid_constant__ CUtensorMap a_map, const _
               if (++s == STAGES) { s = 0; full_par ^= 1; }
               idesc += instr_desc_mx_byte(1);
             }
-            if (ok && ++open == kChunk) close();
+            if (ok && ++open == chunk) close();
           } else {
             if (open != 0) close();
             constexpr uint32_t idesc = instr_desc_pair(kUnit, kFmtE4M3) | kMajor;
@@ -398,7 +403,7 @@ fp8_gemm_kernel(const Args g, const __grid_constant__ CUtensorMap a_map, const _
         if (!wait.cluster(smem_u32(&sfull[f]), f_par, 6)) { ok = false; break; }
         const bool factors = are_factors(f);
         const int n = g1 - kb0 < kStep ? g1 - kb0 : kStep;
-        if (open != 0 && (!factors || open == kChunk) && !take_accumulator()) { ok = false; break; }
+        if (open != 0 && (!factors || open == chunk) && !take_accumulator()) { ok = false; break; }
         if (factors) {
           open++;
         } else {

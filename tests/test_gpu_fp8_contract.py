@@ -40,3 +40,48 @@ def test_binarize_backward_takes_scales_of_either_sign(hb, rows, K, beta, scales
     bound = bound + (fu.BF16 * (np.abs(ref) + bound) if dtype == "bf16" else 0)
     assert (np.abs(got.double().cpu().numpy() - ref) <= bound).all()
     assert torch.equal(got, plain)
+
+
+def values(op):
+    return (op.codes.view(torch.float8_e4m3fn)[:, :op.K].double() * op.scales.double().repeat_interleave(op.block_rows, 0)[:op.rows]
+            .repeat_interleave(128, 1)[:, :op.K])
+
+
+@pytest.mark.parametrize("signs", ["positive", "any"])
+@pytest.mark.parametrize("sizes", ["one", "spread"])
+@pytest.mark.parametrize("out_type", ["fp32", "bf16"])
+@pytest.mark.parametrize("kind,M,N,K", [
+    ("gemm", 512, 512, 8192), ("gemm", 512, 512, 16384), ("gemm", 300, 520, 20000), ("gemm", 2600, 2304, 8192), ("gemm", 2600, 2304, 16384),
+    ("input_grad", 300, 16384, 520), ("input_grad", 2600, 8192, 2304),
+])
+def test_sums_of_long_contractions_do_not_pile_up_truncations(hb, kind, M, N, K, out_type, sizes, signs):
+    """Power-of-two scales: the tensor cores' sums truncate, always towards zero, which shows where nothing cancels and where groups
+    differ in size.  Tiles that are shared along the contraction and tiles that are not.
+    By element: 32 products and the sum so far lose less than 2^-25 of the largest each (33 u / 2), their sum at most a step (2 u), so
+    18.5 u of sum |a w| per 32 elements; a rounding per run and one more for the last.  By norm 4e-6, as the weight gradient: 64
+    instructions a run that lose half a step (u) of a sum growing to its end each, 32 u = 1.9e-6 on average, and as much again for
+    the cut terms of groups that are small beside the sum.  bf16: runs four times as long, 1.6e-5, beside half a step of the result."""
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(M + N + K)
+    L = K if kind == "gemm" else N
+
+    def operand(rows, cols, block_rows, spread_rows, spread_cols):
+        x = torch.randn(rows, cols, generator=gen, device="cuda")
+        x = x.abs() if signs == "positive" else x
+        if sizes == "spread":
+            e = torch.randint(-12, 13, (-(-rows // spread_rows), -(-cols // spread_cols)), generator=gen, device="cuda").float()
+            x *= torch.exp2(e).repeat_interleave(spread_rows, 0)[:rows].repeat_interleave(spread_cols, 1)[:, :cols]
+        return hb.fp8_quantize(x, hb.alloc_fp8_operand(rows, cols, block_rows))
+    A = operand(M, L, 1, M, 128)
+    W = operand(N, K, 128, 128, 128)
+    out = torch.empty(M, N if kind == "gemm" else K, dtype=torch.float32 if out_type == "fp32" else torch.bfloat16, device="cuda")
+    (hb.fp8_gemm if kind == "gemm" else hb.fp8_input_grad)(A, W, out)
+    a, w = values(A), values(W)
+    w = w.t() if kind == "gemm" else w
+    ref, F = a @ w, a.abs() @ w.abs()
+    err = (out.double() - ref).abs()
+    bound = (18.5 * -(-L // 32) + -(-L // 128) + 1) * fu.U * F
+    rounding = fu.BF16 if out_type == "bf16" else 0.0
+    assert (err <= bound + rounding * (ref.abs() + bound)).all()
+    far = (err - rounding * ref.abs()).clamp(min=0)            # beyond half a step of the result: what the sum itself is off
+    assert far.norm() <= (4e-6 if out_type == "fp32" else 1.6e-5) * ref.norm(), float(far.norm() / ref.norm())
