@@ -59,7 +59,7 @@ constexpr int OFF_A = 0, OFF_B = STAGES * kTile, OFF_OUT = STAGES * STAGE, OFF_S
 constexpr int OFF_BAR = OFF_SCALES + kSlots * kSlotBytes;
 constexpr int kBars = 2 * STAGES + 2 * kTurns + 2 + 3 * kSlots + 1;
 constexpr int kScouts = 4, kFlags = 2 * kScouts;                             // words of a slot: one from each scout of both CTAs
-constexpr int OFF_FLAGS = OFF_BAR + kBars * 8, kBytes = OFF_FLAGS + kSlots * kFlags * 4 + 16;
+constexpr int OFF_FLAGS = OFF_BAR + kBars * 8, OFF_SENT = OFF_FLAGS + kSlots * kFlags * 4, kBytes = OFF_SENT + 8 + kScouts * 4 + 8;
 static_assert(kBytes <= 227 * 1024 && TM * TN * 4 <= STAGES * STAGE && kFactorCols + kSlots * kFactorSlot <= 512, "shared and tensor memory");
 
 struct Args {
@@ -95,8 +95,11 @@ fp8_gemm_kernel(const Args g, const __grid_constant__ CUtensorMap a_map, const _
   uint64_t* sfull = scales + kSlots;           // its factors are in both CTAs' tensor memory, and how it is summed is known
   uint64_t* sempty = sfull + kSlots;           // its slot is free in both CTAs
   uint64_t* drained = sempty + kSlots;
-  uint32_t* flags = reinterpret_cast<uint32_t*>(smem + OFF_FLAGS);             // [kSlots][CTA of the pair][scout]: the scales are factors
-  uint32_t* tmem_base_ptr = flags + kSlots * kFlags;
+  // [kSlots][CTA of the pair][scout]: twice the number of the step (from 1), plus 1 where its scales are factors
+  uint32_t* flags = reinterpret_cast<uint32_t*>(smem + OFF_FLAGS);
+  int64_t* issued = reinterpret_cast<int64_t*>(smem + OFF_SENT);               // stages that this CTA's loader has issued, in the end
+  uint32_t* looked = reinterpret_cast<uint32_t*>(issued + 1);                  // steps that each of its scouts has announced
+  uint32_t* tmem_base_ptr = looked + kScouts;
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_base_ptr + 1);
 
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -140,7 +143,7 @@ fp8_gemm_kernel(const Args g, const __grid_constant__ CUtensorMap a_map, const _
   const Waiter wait{g_spin_limit, abort_flag};
   const auto are_factors = [&](uint32_t f) {           // behind sfull; a CTA's scouts have looked at the same scales
     const volatile uint32_t* v = flags + f * kFlags;
-    return (v[0] & v[kScouts]) != 0;
+    return (v[0] & v[kScouts] & 1u) != 0;
   };
 
   if (warp >= kScoutWarp) reg_dec<kRegsScout>();
@@ -153,7 +156,7 @@ fp8_gemm_kernel(const Args g, const __grid_constant__ CUtensorMap a_map, const _
       const uint32_t full0 = mapa_rank(smem_u32(full), lead);
       int s = 0;
       uint32_t round = 0;
-      int64_t issued = 0;
+      int64_t n_issued = 0;
       bool ok = true;
       for (int64_t tile = walker; tile < n_tiles && ok; tile += walkers) {
         int64_t tm, tn;
@@ -166,23 +169,11 @@ fp8_gemm_kernel(const Args g, const __grid_constant__ CUtensorMap a_map, const _
           tma_load_2d_pair(smem + OFF_A + s * kTile, &a_map, kb * kGroup, a_row, bar);
           if (TRANS) tma_load_2d_pair(smem + OFF_B + s * kTile, &w_map, w_at, kb * kGroup, bar);
           else tma_load_2d_pair(smem + OFF_B + s * kTile, &w_map, kb * kGroup, w_at, bar);
-          issued++;
+          n_issued++;
           if (++s == STAGES) { s = 0; round++; }
         }
       }
-      if (!ok || *abort_flag) {
-        // aborted: copies already issued must land before this CTA's shared memory goes away.  The first CTA can watch its
-        // barriers; the second cannot see them and gives its copies a fixed time that is far longer than a copy.
-        if (half == 0) {
-          const int64_t pending = issued < STAGES ? issued : STAGES;
-          for (int64_t q = 1; q <= pending; q++) {
-            const int64_t idx = issued - q;
-            mbar_wait_quiet(&full[idx % STAGES], static_cast<uint32_t>((idx / STAGES) & 1), kDrainPolls);
-          }
-        } else {
-          for (int q = 0; q < 64; q++) __nanosleep(1000);
-        }
-      }
+      *issued = n_issued;
     }
     __syncwarp();
   } else if (warp == kScaleWarp) {
@@ -315,7 +306,7 @@ fp8_gemm_kernel(const Args g, const __grid_constant__ CUtensorMap a_map, const _
     // them when they are needed: a load waits behind the copies in flight, 2 to 3 us for the 192 KB of an SM's stages.)
     const int quarter = warp - kScoutWarp;
     const uint32_t factor_at = tmem_base + (static_cast<uint32_t>(quarter * 32) << 16) + kFactorCols;
-    uint32_t f = 0, f_par = 0;
+    uint32_t f = 0, f_par = 0, n_looked = 0;
     bool ok = true;
     for (int64_t tile = walker; tile < n_tiles && ok; tile += walkers) {
       int64_t tm, tn;
@@ -355,10 +346,11 @@ fp8_gemm_kernel(const Args g, const __grid_constant__ CUtensorMap a_map, const _
         tmem_st_wait();
         tc_fence_before();
         __syncwarp();
+        n_looked++;
         if (lane == 0) {
           // the verdict to both CTAs, and with it that this scout's factors are written
           for (uint32_t c = 0; c < 2; c++)
-            st_async_u32(mapa_rank(smem_u32(flags + f * kFlags + half * kScouts + quarter), lead + c), good ? 1u : 0u,
+            st_async_u32(mapa_rank(smem_u32(flags + f * kFlags + half * kScouts + quarter), lead + c), 2 * n_looked + (good ? 1u : 0u),
                          mapa_rank(smem_u32(&sfull[f]), lead + c));
           if (quarter == 0) mbar_arrive_expect_tx(&sfull[f], kFlags * 4);
           else mbar_arrive(&sfull[f]);
@@ -367,6 +359,7 @@ fp8_gemm_kernel(const Args g, const __grid_constant__ CUtensorMap a_map, const _
         if (++f == kSlots) { f = 0; f_par ^= 1; }
       }
     }
+    if (lane == 0) looked[quarter] = n_looked;
   } else if (warp < kEpilogueWarps) {
     // =========================== epilogue (both CTAs) ===========================
     reg_inc<kRegsEpilogue>();
@@ -454,12 +447,17 @@ fp8_gemm_kernel(const Args g, const __grid_constant__ CUtensorMap a_map, const _
     }
     __syncwarp();
   }
-  // No CTA may leave while another can still reach into it (the MMAs read the second CTA's shared memory and write its tensor
-  // memory; copies, scouts and epilogue warps signal barriers of both; partial sums are read by the whole cluster).
-  __syncwarp();
-  tc_fence_before();
-  __syncthreads();
-  cluster_sync_all();
+  // The MMAs read the second CTA's shared memory and write its tensor memory; copies, scouts and epilogue warps signal barriers of
+  // both; partial sums are read by the whole cluster.
+  leave_cluster(abort_flag, 2 * g.parts, [&](uint32_t me) {
+    for (uint32_t q = 0; q < kScouts; q++) {
+      const uint32_t n = looked[q];
+      for (uint32_t i = n > kSlots ? n - kSlots : 0; i < n; i++)
+        for (uint32_t c = 0; c < 2; c++)
+          wait_word(mapa_rank(smem_u32(flags + i % kSlots * kFlags + (me & 1) * kScouts + q), (me & ~1u) + c), ~1u, 2 * (i + 1));
+    }
+    if ((me & 1) == 0) drain_pair_copies<STAGES>(full, *issued, ld_cluster_s64(mapa_rank(smem_u32(issued), me + 1)), STAGE);
+  });
   if (warp == kMmaWarp) {
     tc_fence_after();
     tmem_dealloc_pair(tmem_base, 512);

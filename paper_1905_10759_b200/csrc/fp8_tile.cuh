@@ -222,6 +222,19 @@ __device__ __forceinline__ void stage_part(unsigned char* base, const uint64_t (
     *reinterpret_cast<float4*>(base + part_offset<TN>(row, (p < 16 ? c0 : c1) / 4 + p % 16)) = make_float4(v[0], v[1], v[2], v[3]);
   }
 }
+__device__ __forceinline__ uint32_t ld_cluster_u32(uint32_t addr) {
+  uint32_t v;
+  asm volatile("ld.volatile.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(addr) : "memory");
+  return v;
+}
+__device__ __forceinline__ int64_t ld_cluster_s64(uint32_t addr) {
+  int64_t v;
+  asm volatile("ld.volatile.shared::cluster.s64 %0, [%1];" : "=l"(v) : "r"(addr) : "memory");
+  return v;
+}
+__device__ __forceinline__ void st_cluster_u32(uint32_t addr, uint32_t v) {
+  asm volatile("st.volatile.shared::cluster.u32 [%0], %1;" ::"r"(addr), "r"(v) : "memory");
+}
 __device__ __forceinline__ float4 ld_cluster16(uint32_t addr) {
   float4 v;
   asm volatile("ld.shared::cluster.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr));
@@ -279,6 +292,43 @@ int choose_parts(Kernel kernel, int threads, int bytes, std::atomic<int> (&known
     if (tiles <= n - 1) return parts;
   }
   return 1;
+}
+
+// ---- the end of a kernel
+// Returns when no CTA of the cluster reaches into this one any more; every thread of every CTA comes here behind its role.  Where a
+// wait gave up in one of them, copies and announcements may still be on their way: drain, which every CTA's first thread then runs
+// while all of them are there, waits for those of its CTA, whose number it knows by then (each wait bounded as the others).
+template <typename Drain>
+__device__ __forceinline__ void leave_cluster(volatile int* abort_flag, uint32_t ctas, Drain drain) {
+  __syncwarp();
+  tc_fence_before();
+  __syncthreads();
+  if (*abort_flag != 0 && threadIdx.x < ctas) st_cluster_u32(mapa_rank(smem_u32(const_cast<int*>(abort_flag)), threadIdx.x), 1u);
+  __syncwarp();
+  cluster_sync_all();
+  if (*abort_flag != 0) {                               // the same in every CTA
+    if (threadIdx.x == 0) drain(cluster_ctarank());     // read again: kept from the start it costs registers that spill
+    __syncwarp();
+    __syncthreads();
+    cluster_sync_all();
+  }
+}
+// Copies that both CTAs of a pair issue, STAGES ahead at most, complete on the first one's barriers, `bytes` from each and one arrival,
+// which expects both.  The first CTA waits for the last of them: issued and other are the copies of the two.
+template <int STAGES>
+__device__ __forceinline__ void drain_pair_copies(uint64_t* full, int64_t issued, int64_t other, uint32_t bytes) {
+  const int64_t last = issued > other ? issued : other;
+  for (int64_t i = last > STAGES ? last - STAGES : 0; i < last; i++) {
+    uint64_t* bar = &full[i % STAGES];
+    if (i >= issued) mbar_arrive_expect_tx(bar, bytes);              // the other CTA went further
+    else if (i >= other) mbar_complete_tx(bar, bytes);               // this one did
+    mbar_wait_quiet(bar, static_cast<uint32_t>((i / STAGES) & 1), kDrainPolls);
+  }
+}
+// A word that st_async_u32 is bringing to this address of the cluster.
+__device__ __forceinline__ void wait_word(uint32_t cluster_addr, uint32_t mask, uint32_t value) {
+  for (uint32_t it = 0; it < kDrainPolls; it++)
+    if ((ld_cluster_u32(cluster_addr) & mask) == value) return;
 }
 
 // Output tiles are walked in blocks of eight rows of tiles, column by column, so that the tiles in flight at one time cover about as

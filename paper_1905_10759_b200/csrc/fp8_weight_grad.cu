@@ -39,7 +39,7 @@ constexpr int kSlots = 16;                     // stages of scales
 constexpr int OFF_A = 0, OFF_B = STAGES * kOperand, OFF_CODES = 2 * STAGES * kOperand, OFF_OUT = OFF_CODES + STAGES * kCodes;
 constexpr int OFF_SCALES = OFF_OUT + kEpilogueWarps * kStoreBytes, OFF_BAR = OFF_SCALES + kSlots * ROWS * 4;
 constexpr int kBars = 6 * STAGES + 2 * kSlots + 5;
-constexpr int kBytes = OFF_BAR + kBars * 8 + 16 + STAGES * 4;
+constexpr int OFF_SENT = OFF_BAR + kBars * 8, kBytes = OFF_SENT + 8 + 4 + STAGES * 4 + 8;
 // An accumulator in tensor memory takes 512 rows, the epilogue adds it to fp32 registers: the tensor cores' additions truncate, always
 // towards zero, and with 8192 rows of sizes from 2^-8 to 2^8 in one accumulator the result was 9e-6 off.
 constexpr int kChunkStages = 512 / ROWS;
@@ -68,9 +68,11 @@ fp8_weight_grad_kernel(const Args g, const __grid_constant__ CUtensorMap gy_map,
   uint64_t* tfull = sempty + kSlots;
   uint64_t* tempty = tfull + 2;
   uint64_t* drained = tempty + 2;
-  uint32_t* tmem_base_ptr = reinterpret_cast<uint32_t*>(drained + 1);
+  int64_t* issued = reinterpret_cast<int64_t*>(smem + OFF_SENT);     // stages that this CTA's loader has issued, in the end
+  uint32_t* announced = reinterpret_cast<uint32_t*>(issued + 1);     // second CTA: stages that it has announced, in the end
+  uint32_t* told = announced + 1;              // first CTA, [STAGES]: where the announcements land, the number of the stage (from 1)
+  uint32_t* tmem_base_ptr = told + STAGES;
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_base_ptr + 1);
-  uint32_t* told = tmem_base_ptr + 2;          // first CTA, [STAGES]: where the second one's announcements land
 
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const uint32_t rank = cluster_ctarank(), lead = rank & ~1u, half = rank & 1u;
@@ -116,7 +118,7 @@ fp8_weight_grad_kernel(const Args g, const __grid_constant__ CUtensorMap gy_map,
       const uint32_t afull0 = mapa_rank(smem_u32(afull), lead);
       int s = 0, c = 0;
       uint32_t par = 1;                                  // the first round waits for nobody
-      int64_t issued = 0;
+      int64_t n_issued = 0;
       bool ok = true;
       for (int64_t tile = walker; tile < n_tiles && ok; tile += walkers) {
         int64_t tm, tn;
@@ -134,21 +136,11 @@ fp8_weight_grad_kernel(const Args g, const __grid_constant__ CUtensorMap gy_map,
           unsigned char* a = smem + OFF_A + s * kOperand;
           tma_load_2d_pair(a, &gy_map, n_at, st * ROWS, afull0 + s * 8);
           tma_load_2d_pair(a + kChunkBytes, &gy_map, n_at + 64, st * ROWS, afull0 + s * 8);
-          issued++;
+          n_issued++;
           if (++s == STAGES) { s = 0; par ^= 1; }
         }
       }
-      if (!ok || *abort_flag) {
-        // aborted: copies already issued must land before this CTA's shared memory goes away (the second CTA cannot see the
-        // barriers of its copies of gy and gives them a fixed time that is far longer than a copy)
-        for (int64_t q = 1; q <= (issued < STAGES ? issued : STAGES); q++) {
-          const int64_t i = issued - q;
-          mbar_wait_quiet(&cfull[i % (2 * STAGES)], static_cast<uint32_t>((i / (2 * STAGES)) & 1), kDrainPolls);
-          if (half == 0) mbar_wait_quiet(&afull[i % STAGES], static_cast<uint32_t>((i / STAGES) & 1), kDrainPolls);
-        }
-        if (half != 0)
-          for (int q = 0; q < 64; q++) __nanosleep(1000);
-      }
+      *issued = n_issued;
     }
     __syncwarp();
   } else if (warp == kScaleWarp) {
@@ -178,14 +170,15 @@ fp8_weight_grad_kernel(const Args g, const __grid_constant__ CUtensorMap gy_map,
     // =========================== announcements (second CTA) ===========================
     if (half != 0 && elect_one()) {
       const uint32_t bfull0 = mapa_rank(smem_u32(bfull), lead), told0 = mapa_rank(smem_u32(told), lead);
-      uint32_t s = 0, par = 0;
+      uint32_t s = 0, par = 0, n = 0;
       bool ok = true;
       for (int64_t tile = walker; tile < n_tiles && ok; tile += walkers)
         for (int st = s0; st < s1; st++) {
           if (!wait(smem_u32(&bdone[s]), par, 7)) { ok = false; break; }
-          st_async_u32(told0 + s * 4, 1u, bfull0 + s * 8);
+          st_async_u32(told0 + s * 4, ++n, bfull0 + s * 8);
           if (++s == STAGES) { s = 0; par ^= 1; }
         }
+      *announced = n;
     }
     __syncwarp();
   } else if (warp >= kConvertWarp) {
@@ -193,7 +186,7 @@ fp8_weight_grad_kernel(const Args g, const __grid_constant__ CUtensorMap gy_map,
     // Four warps per stage, the other four on the next one: a warp's waits and its fence come once per four items of work.
     const int me = tid - kConvertWarp * 32 & 127;
     const uint32_t mine = (warp - kConvertWarp) / 4;
-    uint64_t* converted = half == 0 ? bfull : bdone;
+    const uint32_t converted = smem_u32(half == 0 ? bfull : bdone);
     const int q = me & 7;                                // 16 codes from column 16 q, rows me / 8 + 16 i
     uint32_t s = 0, c = 0, c_par = 0, f = 0, f_par = 0, turn = 0;
     bool ok = true;
@@ -227,7 +220,7 @@ fp8_weight_grad_kernel(const Args g, const __grid_constant__ CUtensorMap gy_map,
           fence_async_proxy();                           // the stores are the tensor core's to read
           __syncwarp();
           if (lane == 0) {
-            mbar_arrive(&converted[s]);
+            mbar_arrive_a(converted + s * 8);
             mbar_arrive(&sempty[f]);
           }
         }
@@ -323,11 +316,17 @@ fp8_weight_grad_kernel(const Args g, const __grid_constant__ CUtensorMap gy_map,
       finish_parts<TN>(g.out, smem, part, g.parts, half, tm * 2 * TM + half * TM, tn * TN, tid, kEpilogueWarps * 32);
     }
   }
-  // No CTA may leave while another can still reach into it.
-  __syncwarp();
-  tc_fence_before();
-  __syncthreads();
-  cluster_sync_all();
+  leave_cluster(abort_flag, 2 * g.parts, [&](uint32_t me) {
+    const int64_t n = *issued;
+    for (int64_t i = n > STAGES ? n - STAGES : 0; i < n; i++)
+      mbar_wait_quiet(&cfull[i % (2 * STAGES)], static_cast<uint32_t>((i / (2 * STAGES)) & 1), kDrainPolls);
+    if ((me & 1) == 0) {
+      drain_pair_copies<STAGES>(afull, n, ld_cluster_s64(mapa_rank(smem_u32(issued), me + 1)), kOperand);
+    } else {
+      const uint32_t m = *announced;
+      for (uint32_t i = m > STAGES ? m - STAGES : 0; i < m; i++) wait_word(mapa_rank(smem_u32(told + i % STAGES), me - 1), ~0u, i + 1);
+    }
+  });
   if (warp == kMmaWarp) {
     tc_fence_after();
     tmem_dealloc_pair(tmem_base, 512);
