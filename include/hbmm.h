@@ -401,7 +401,8 @@ hbmm_status hbmm_conv_im2col_static(const void *x, int32_t x_dtype, const hbmm_c
  *            Entry (r / block_rows, k / 128) belongs to element (r, k); entries behind the last group are ignored.
  *   block_rows : 1 (activations, gradients: a scale per group of 128 consecutive row elements) or 128 (weights: a scale
  *            per block of 128 x 128 elements).
- * rows and K are below 2^31.  The last group of a row and the last block of a column may be short.
+ * rows and K are below 2^31; rows of this and of the other matrices of these calls are less than 2^40 bytes apart.  The last
+ * group of a row and the last block of a column may be short.
  */
 typedef struct {
   int64_t rows;

@@ -10,7 +10,7 @@ namespace {
 
 constexpr int64_t kGroup = 128;
 constexpr int64_t kMaxExtent = int64_t{1} << 31;        // rows and columns are tensor-copy coordinates
-constexpr int64_t kMaxPitch = int64_t{1} << 40;         // bytes between rows that a tensor map can hold
+constexpr int64_t kMaxPitch = int64_t{1} << 40;         // bytes between rows that a tensor map can hold; every matrix's here
 
 inline bool on16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 inline int64_t up(int64_t v, int64_t a) { return (v + a - 1) / a * a; }
@@ -29,10 +29,11 @@ hbmm_status check_operand(const hbmm_fp8_operand* op, int32_t block_rows = 0) {
 
 Fp8View view_of(const hbmm_fp8_operand* op) { return {op->codes, op->scales, op->rows, op->K, op->ld_codes, op->ld_scales}; }
 
-// A matrix whose rows start on 16-byte boundaries.
-hbmm_status check_rows(const void* p, int64_t cols, int64_t ld, int64_t size) {
+// A matrix whose rows start on 16-byte boundaries, or wherever its elements may.
+hbmm_status check_rows(const void* p, int64_t cols, int64_t ld, int64_t size, bool rows16 = true) {
   if (!p || ld < cols) return HBMM_ERR_INVALID_ARG;
   if (ld >= kMaxPitch / size) return HBMM_ERR_UNSUPPORTED;
+  if (!rows16) return reinterpret_cast<uintptr_t>(p) % size == 0 ? HBMM_OK : HBMM_ERR_ALIGNMENT;
   return on16(p) && ld * size % 16 == 0 ? HBMM_OK : HBMM_ERR_ALIGNMENT;
 }
 inline int64_t size_of(int32_t dtype) { return dtype == HBMM_BF16 ? 2 : 4; }
@@ -56,10 +57,10 @@ hbmm_status hbmm_fp8_operand_bytes(int64_t rows, int64_t K, int32_t block_rows, 
 
 hbmm_status hbmm_fp8_quantize(const void* x, int32_t x_dtype, int64_t rows, int64_t K, int64_t ldx, const hbmm_fp8_operand* out,
                               void* stream) {
-  const hbmm_status st = check_operand(out);
+  hbmm_status st = check_operand(out);
   if (st != HBMM_OK) return st;
-  if (!x || !valid_dtype(x_dtype) || rows != out->rows || K != out->K || ldx < K) return HBMM_ERR_INVALID_ARG;
-  if (reinterpret_cast<uintptr_t>(x) % size_of(x_dtype) != 0) return HBMM_ERR_ALIGNMENT;
+  if (!valid_dtype(x_dtype) || rows != out->rows || K != out->K) return HBMM_ERR_INVALID_ARG;
+  if ((st = check_rows(x, K, ldx, size_of(x_dtype), false)) != HBMM_OK) return st;
   return status_of(launch_fp8_quantize(x, x_dtype == HBMM_BF16, rows, K, ldx, out->codes, out->ld_codes, out->scales, out->ld_scales,
                                        out->block_rows != 1, static_cast<cudaStream_t>(stream)));
 }
@@ -100,11 +101,11 @@ hbmm_status hbmm_fp8_weight_grad(const void* gy, int32_t gy_dtype, int64_t N, in
 
 hbmm_status hbmm_fp8_binarize_backward(const hbmm_fp8_operand* X, const void* gy, int32_t dtype, int64_t ldg, int32_t beta, void* gx,
                                        int64_t ldo, void* stream) {
-  const hbmm_status st = check_operand(X, 1);
+  hbmm_status st = check_operand(X, 1);
   if (st != HBMM_OK) return st;
-  if (!gy || !gx || beta < 1 || !valid_dtype(dtype) || ldg < X->K || ldo < X->K) return HBMM_ERR_INVALID_ARG;
-  if (reinterpret_cast<uintptr_t>(gy) % size_of(dtype) != 0 || reinterpret_cast<uintptr_t>(gx) % size_of(dtype) != 0)
-    return HBMM_ERR_ALIGNMENT;
+  if (beta < 1 || !valid_dtype(dtype)) return HBMM_ERR_INVALID_ARG;
+  if ((st = check_rows(gy, X->K, ldg, size_of(dtype), false)) != HBMM_OK) return st;
+  if ((st = check_rows(gx, X->K, ldo, size_of(dtype), false)) != HBMM_OK) return st;
   return status_of(launch_fp8_binarize_backward(view_of(X), gy, dtype == HBMM_BF16, ldg, beta, gx, ldo, static_cast<cudaStream_t>(stream)));
 }
 

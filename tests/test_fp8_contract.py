@@ -89,3 +89,16 @@ def test_a_kernel_that_gives_up_waits_for_its_pair_s_copies(tmp_path):
 def test_no_kernel_leaves_by_the_clock(name):
     code = source(name)
     assert "nanosleep" not in code and "leave_cluster(" in code and "drain_pair_copies<STAGES>(" in code
+
+
+def test_rows_too_far_apart_are_refused_by_every_argument():
+    """Fake addresses, never dereferenced."""
+    import ctypes
+    from paper_1905_10759_b200 import hbmm
+    lib, by, P = hbmm._lib, ctypes.byref, ctypes.c_void_p
+    x = hbmm.hbmm_fp8_operand(8, 256, 0x1000, 256, 0x2000, 4, 1, 0)
+    for ld in (1 << 62, 1 << 60, 1 << 39):                 # fp32: 2^64, 2^62, 2^41 bytes
+        for dtype in (0, 1):
+            assert lib.hbmm_fp8_quantize(P(0x4000), dtype, 8, 256, ld, by(x), None) == hbmm.ERR_UNSUPPORTED
+            assert lib.hbmm_fp8_binarize_backward(by(x), P(0x4000), dtype, ld, 32, P(0x8000), 256, None) == hbmm.ERR_UNSUPPORTED
+            assert lib.hbmm_fp8_binarize_backward(by(x), P(0x4000), dtype, 256, 32, P(0x8000), ld, None) == hbmm.ERR_UNSUPPORTED
