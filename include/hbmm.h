@@ -509,6 +509,11 @@ hbmm_status hbmm_clear_device_error(void);
  */
 hbmm_status hbmm_debug_set_wait_limit(uint32_t polls);
 hbmm_status hbmm_debug_expire_wait(void *stream);
+/*
+ * The same with the waits of one kernel family: 300 (the call above), 400 (products of 8-bit operands: code 409), 500 (the weight
+ * gradient from one: code 509).  Errors: INVALID_ARG (family), CUDA.
+ */
+hbmm_status hbmm_debug_expire_wait_of(int32_t family, void *stream);
 
 /*
  * Measurement aid: a register-only arithmetic loop that times the issue rate of one unit -- kind 0: 32-bit

@@ -573,6 +573,18 @@ hbmm_status hbmm_debug_expire_wait(void* stream) {
   return launch_wait_expiry_selftest(static_cast<cudaStream_t>(stream)) == cudaSuccess ? HBMM_OK : HBMM_ERR_CUDA;
 }
 
+hbmm_status hbmm_debug_expire_wait_of(int32_t family, void* stream) {
+  const cudaStream_t s = static_cast<cudaStream_t>(stream);
+  cudaError_t e;
+  switch (family) {
+    case 300: e = launch_wait_expiry_selftest(s); break;
+    case 400: e = fp8_gemm_expire_wait(s); break;
+    case 500: e = fp8_weight_grad_expire_wait(s); break;
+    default: return HBMM_ERR_INVALID_ARG;
+  }
+  return e == cudaSuccess ? HBMM_OK : HBMM_ERR_CUDA;
+}
+
 hbmm_status hbmm_bench_alu_rate(int32_t kind, int32_t blocks, int32_t iters, uint32_t* sink, int64_t* ops, void* stream) {
   if (kind < 0 || kind > 2 || blocks <= 0 || iters <= 0 || !sink) return HBMM_ERR_INVALID_ARG;
   return launch_alu_rate(kind, blocks, iters, sink, ops, static_cast<cudaStream_t>(stream)) == cudaSuccess ? HBMM_OK : HBMM_ERR_CUDA;

@@ -508,6 +508,8 @@ cudaError_t launch_fp8_gemm(const Fp8View& A, const Fp8View& W, bool transposed,
   return transposed ? launch<true>(g, A, W, dev, sms, stream) : launch<false>(g, A, W, dev, sms, stream);
 }
 
+cudaError_t fp8_gemm_expire_wait(cudaStream_t stream) { return launch_wait_expiry(stream); }
+
 cudaError_t fp8_gemm_health(int op, int* value) {
   switch (op) {
     case kHealthRead: return umma::read_error_word(value);

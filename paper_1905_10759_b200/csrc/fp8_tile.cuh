@@ -331,6 +331,24 @@ __device__ __forceinline__ void wait_word(uint32_t cluster_addr, uint32_t mask, 
     if ((ld_cluster_u32(cluster_addr) & mask) == value) return;
 }
 
+// Test only: a thread each in two blocks waits, in the two ways that the kernels' roles do, on a barrier that nobody arrives at and
+// that guards nothing (no copy, no MMA in flight).  The waits run out after the limit in force and record code 9.
+static __global__ void wait_expiry_kernel() {
+  __shared__ uint64_t bar;
+  __shared__ int flag;
+  if (threadIdx.x != 0) return;
+  mbar_init(&bar, 1);
+  flag = 0;
+  asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  const Waiter wait{g_spin_limit, &flag};
+  if (blockIdx.x == 0) wait(smem_u32(&bar), 0, 9);
+  else wait.cluster(smem_u32(&bar), 0, 9);
+}
+inline cudaError_t launch_wait_expiry(cudaStream_t stream) {
+  wait_expiry_kernel<<<2, 32, 0, stream>>>();
+  return cudaGetLastError();
+}
+
 // Output tiles are walked in blocks of eight rows of tiles, column by column, so that the tiles in flight at one time cover about as
 // many rows of one operand as of the other (fewest bytes read for the products of a wave).
 __device__ __forceinline__ void tile_at(int64_t i, int64_t tiles_m, int64_t tiles_n, int64_t* tm, int64_t* tn) {

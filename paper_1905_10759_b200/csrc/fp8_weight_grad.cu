@@ -373,6 +373,8 @@ cudaError_t launch_fp8_weight_grad(const void* gy, int64_t N, int64_t ldg, const
                             kBytes, stream, g, gy_map, x_map);
 }
 
+cudaError_t fp8_weight_grad_expire_wait(cudaStream_t stream) { return launch_wait_expiry(stream); }
+
 cudaError_t fp8_weight_grad_health(int op, int* value) {
   switch (op) {
     case kHealthRead: return umma::read_error_word(value);

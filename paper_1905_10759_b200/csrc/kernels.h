@@ -252,6 +252,8 @@ bool fp8_gemv_supported(const Fp8View& A);
 cudaError_t launch_fp8_gemv(const Fp8View& A, const Fp8View& W, void* C, bool c_bf16, int64_t ldc, cudaStream_t stream);
 cudaError_t fp8_gemm_health(int op, int* value);
 cudaError_t fp8_weight_grad_health(int op, int* value);
+cudaError_t fp8_gemm_expire_wait(cudaStream_t stream);
+cudaError_t fp8_weight_grad_expire_wait(cudaStream_t stream);
 cudaError_t launch_fp8_weight_grad(const void* gy, int64_t N, int64_t ldg, const Fp8View& X, const float* base, int64_t ld_base, float* gw,
                                    int64_t ldw, cudaStream_t stream);
 cudaError_t launch_fp8_binarize_backward(const Fp8View& X, const void* gy, bool bf16, int64_t ldg, int64_t beta, void* gx, int64_t ldo,

@@ -44,7 +44,8 @@ EXPORTS = [
     "hbmm_gemm_partials", "hbmm_conv_workspace_bytes", "hbmm_conv_im2col", "hbmm_status_string",
     "hbmm_version", "hbmm_conv_im2col_static", "hbmm_last_device_error", "hbmm_conv_im2col_ex",
     "hbmm_binarize_backward", "hbmm_gemm_binarize_next", "hbmm_binarize_dense",
-    "hbmm_clear_device_error", "hbmm_debug_set_wait_limit", "hbmm_debug_expire_wait", "hbmm_bench_alu_rate",
+    "hbmm_clear_device_error", "hbmm_debug_set_wait_limit", "hbmm_debug_expire_wait", "hbmm_debug_expire_wait_of",
+    "hbmm_bench_alu_rate",
     "hbmm_gemm_fused", "hbmm_conv_im2col_fused",
     "hbmm_fp8_operand_bytes", "hbmm_fp8_quantize", "hbmm_fp8_gemm", "hbmm_fp8_input_grad", "hbmm_fp8_weight_grad",
     "hbmm_fp8_binarize_backward",
@@ -311,6 +312,8 @@ _lib.hbmm_debug_set_wait_limit.argtypes = [ctypes.c_uint32]
 _lib.hbmm_debug_set_wait_limit.restype = _i32
 _lib.hbmm_debug_expire_wait.argtypes = [_vp]
 _lib.hbmm_debug_expire_wait.restype = _i32
+_lib.hbmm_debug_expire_wait_of.argtypes = [_i32, _vp]
+_lib.hbmm_debug_expire_wait_of.restype = _i32
 _lib.hbmm_bench_alu_rate.argtypes = [_i32, _i32, _i32, _vp, _P(_i64), _vp]
 _lib.hbmm_bench_alu_rate.restype = _i32
 
@@ -328,6 +331,11 @@ def debug_set_wait_limit(polls: int) -> None:
 def debug_expire_wait(stream=None) -> None:
     """hbmm_debug_expire_wait: one thread waits on a barrier nobody arrives at until the limit runs out."""
     _check(_lib.hbmm_debug_expire_wait(_stream(stream)), "hbmm_debug_expire_wait")
+
+
+def debug_expire_wait_of(family: int, stream=None) -> None:
+    """hbmm_debug_expire_wait_of: the same with the waits of a kernel family (300, 400, 500)."""
+    _check(_lib.hbmm_debug_expire_wait_of(family, _stream(stream)), "hbmm_debug_expire_wait_of")
 
 
 ALU_POPC, ALU_FADD, ALU_FFMA = 0, 1, 2

@@ -102,3 +102,9 @@ def test_rows_too_far_apart_are_refused_by_every_argument():
             assert lib.hbmm_fp8_quantize(P(0x4000), dtype, 8, 256, ld, by(x), None) == hbmm.ERR_UNSUPPORTED
             assert lib.hbmm_fp8_binarize_backward(by(x), P(0x4000), dtype, ld, 32, P(0x8000), 256, None) == hbmm.ERR_UNSUPPORTED
             assert lib.hbmm_fp8_binarize_backward(by(x), P(0x4000), dtype, 256, 32, P(0x8000), ld, None) == hbmm.ERR_UNSUPPORTED
+
+
+@pytest.mark.parametrize("family", [0, 100, 200, 309, 600, -400])
+def test_families_without_a_wait_to_expire_are_refused(family):
+    from paper_1905_10759_b200 import hbmm
+    assert hbmm._lib.hbmm_debug_expire_wait_of(family, None) == hbmm.ERR_INVALID_ARG
