@@ -423,7 +423,9 @@ hbmm_status hbmm_fp8_operand_bytes(int64_t rows, int64_t K, int32_t block_rows, 
  * Quantization to 8 bits.  Per group or block: amax the largest finite magnitude, scale = the smallest power of two with
  * amax / scale <= 448 (the largest e4m3 value), at least 2^-117; code = x / scale rounded to nearest even.  x / scale and
  * code * scale are exact for a power of two, and code * scale is a bf16 number: the backward products below read it
- * without another rounding.  NaN and infinities become NaN codes and do not count in amax.  -0 becomes +0; a negative
+ * without another rounding.  (Elements above 1.9375 * 2^127 round to 2^128, which no bf16 or fp32 holds: infinite where code *
+ * scale is formed, in the weight gradient and in hbmm_fp8_binarize_backward; the other products never form it.)
+ * NaN and infinities become NaN codes and do not count in amax.  -0 becomes +0; a negative
  * element that rounds to zero keeps its sign bit (hbmm_fp8_binarize_backward takes the element's sign from there).
  * x: device, [rows, ldx] of x_dtype, ldx >= K, aligned to its element (16-byte aligned rows take vector loads).
  * out: host descriptor, its buffers filled.  Errors: INVALID_ARG, UNSUPPORTED (block_rows, sizes), ALIGNMENT, CUDA.

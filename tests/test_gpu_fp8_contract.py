@@ -85,3 +85,46 @@ def test_sums_of_long_contractions_do_not_pile_up_truncations(hb, kind, M, N, K,
     assert (err <= bound + rounding * (ref.abs() + bound)).all()
     far = (err - rounding * ref.abs()).clamp(min=0)            # beyond half a step of the result: what the sum itself is off
     assert far.norm() <= (4e-6 if out_type == "fp32" else 1.6e-5) * ref.norm(), float(far.norm() / ref.norm())
+
+
+@pytest.mark.parametrize("M", [1, 40])
+def test_the_largest_numbers(hb, M):
+    """Above 1.9375 * 2^127 an element rounds to a code times scale of 2^128: the products take code and scale apart and give its
+    multiple; the weight gradient, which forms it, is infinite there and nowhere else."""
+    x = torch.ones(M, 256, device="cuda")
+    x[:, 3] = 3.4e38
+    X = hb.fp8_quantize(x, hb.alloc_fp8_operand(M, 256))
+    w = torch.zeros(24, 256, device="cuda")
+    w[:, 3] = torch.arange(24, device="cuda") * 2.0 ** -100
+    W = hb.fp8_quantize(w, hb.alloc_fp8_operand(24, 256, 128))
+    y = hb.fp8_gemm(X, W, torch.empty(M, 24, device="cuda"))
+    assert torch.equal(y.double(), (values(W)[:, 3] * 2.0 ** 128).expand(M, 24))          # of the weights as their codes hold them
+    gw = hb.fp8_weight_grad(torch.ones(M, 24, dtype=torch.bfloat16, device="cuda"), X, torch.empty(24, 256, device="cuda"))
+    want = torch.full((24, 256), float(M), device="cuda")
+    want[:, :128] = 0.0                                    # ones beside 2^128: below the smallest code of its scale
+    want[:, 3] = float("inf")
+    assert torch.equal(gw, want)
+
+
+@pytest.mark.parametrize("M", [3, 40, 300])
+@pytest.mark.parametrize("scale", [float("nan"), float("inf"), 0.0, 2.0 ** -130, -2.0, 3.0])
+def test_a_scale_matters_to_its_group_alone(hb, M, scale):
+    """One group's scale in A, one block's in W: every other element of the product is what it was with ordinary ones, every
+    element of theirs is the definition's, NaN and infinity included."""
+    rng = np.random.default_rng(M)
+    A, a, ca, sa = fu.held(rng.integers(1, 9, (M, 700)).astype(np.float32), 1)
+    W, w, cw, sw = fu.held(rng.integers(1, 9, (260, 700)).astype(np.float32), 128)
+    plain = hb.fp8_gemm(A, W, torch.empty(M, 260, device="cuda")).cpu().numpy()
+    A.scales[M // 2, 4] = scale
+    W.scales[1, 2] = scale
+    got = hb.fp8_gemm(A, W, torch.empty(M, 260, device="cuda")).cpu().numpy()
+    sa[M // 2, 4] = sw[1, 2] = np.float32(scale)
+    with np.errstate(all="ignore"):
+        ref = fu.values(ca, sa, 1) @ fu.values(cw, sw, 128).T
+    same = np.ones_like(plain, dtype=bool)
+    same[M // 2] = False
+    same[:, 128:256] = False
+    assert np.array_equal(got[same], plain[same])
+    assert np.array_equal(np.isnan(got), np.isnan(ref)) and np.array_equal(np.isinf(got), np.isinf(ref))
+    fin = np.isfinite(ref)
+    assert np.allclose(got[fin], ref[fin], rtol=1e-6, atol=0)
