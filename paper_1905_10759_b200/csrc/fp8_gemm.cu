@@ -59,6 +59,9 @@ constexpr int OFF_A = 0, OFF_B = STAGES * kTile, OFF_OUT = STAGES * STAGE, OFF_S
 constexpr int OFF_BAR = OFF_SCALES + kSlots * kSlotBytes;
 constexpr int kBars = 2 * STAGES + 2 * kTurns + 2 + 3 * kSlots + 1;
 constexpr int kScouts = 4, kFlags = 2 * kScouts;                             // words of a slot: one from each scout of both CTAs
+// In such a word.  Tested by the sign: with the lowest bit in its place, masked out, scales of any value took 580 us at 8192^3, not 562
+// (the same work otherwise; by how the compiler arranged the epilogue).
+constexpr uint32_t kNoFactors = 1u << 31;
 constexpr int OFF_FLAGS = OFF_BAR + kBars * 8, OFF_SENT = OFF_FLAGS + kSlots * kFlags * 4, kBytes = OFF_SENT + 8 + kScouts * 4 + 8;
 static_assert(kBytes <= 227 * 1024 && TM * TN * 4 <= STAGES * STAGE && kFactorCols + kSlots * kFactorSlot <= 512, "shared and tensor memory");
 
@@ -95,7 +98,7 @@ fp8_gemm_kernel(const Args g, const __grid_constant__ CUtensorMap a_map, const _
   uint64_t* sfull = scales + kSlots;           // its factors are in both CTAs' tensor memory, and how it is summed is known
   uint64_t* sempty = sfull + kSlots;           // its slot is free in both CTAs
   uint64_t* drained = sempty + kSlots;
-  // [kSlots][CTA of the pair][scout]: twice the number of the step (from 1), plus 1 where its scales are factors
+  // [kSlots][CTA of the pair][scout]: the number of the step (from 1), and the topmost bit where its scales are no factors
   uint32_t* flags = reinterpret_cast<uint32_t*>(smem + OFF_FLAGS);
   int64_t* issued = reinterpret_cast<int64_t*>(smem + OFF_SENT);               // stages that this CTA's loader has issued, in the end
   uint32_t* looked = reinterpret_cast<uint32_t*>(issued + 1);                  // steps that each of its scouts has announced
@@ -143,7 +146,7 @@ fp8_gemm_kernel(const Args g, const __grid_constant__ CUtensorMap a_map, const _
   const Waiter wait{g_spin_limit, abort_flag};
   const auto are_factors = [&](uint32_t f) {           // behind sfull; a CTA's scouts have looked at the same scales
     const volatile uint32_t* v = flags + f * kFlags;
-    return (v[0] & v[kScouts] & 1u) != 0;
+    return static_cast<int32_t>(v[0] | v[kScouts]) >= 0;
   };
 
   if (warp >= kScoutWarp) reg_dec<kRegsScout>();
@@ -350,7 +353,7 @@ fp8_gemm_kernel(const Args g, const __grid_constant__ CUtensorMap a_map, const _
         if (lane == 0) {
           // the verdict to both CTAs, and with it that this scout's factors are written
           for (uint32_t c = 0; c < 2; c++)
-            st_async_u32(mapa_rank(smem_u32(flags + f * kFlags + half * kScouts + quarter), lead + c), 2 * n_looked + (good ? 1u : 0u),
+            st_async_u32(mapa_rank(smem_u32(flags + f * kFlags + half * kScouts + quarter), lead + c), n_looked | (good ? 0u : kNoFactors),
                          mapa_rank(smem_u32(&sfull[f]), lead + c));
           if (quarter == 0) mbar_arrive_expect_tx(&sfull[f], kFlags * 4);
           else mbar_arrive(&sfull[f]);
@@ -454,7 +457,7 @@ fp8_gemm_kernel(const Args g, const __grid_constant__ CUtensorMap a_map, const _
       const uint32_t n = looked[q];
       for (uint32_t i = n > kSlots ? n - kSlots : 0; i < n; i++)
         for (uint32_t c = 0; c < 2; c++)
-          wait_word(mapa_rank(smem_u32(flags + i % kSlots * kFlags + (me & 1) * kScouts + q), (me & ~1u) + c), ~1u, 2 * (i + 1));
+          wait_word(mapa_rank(smem_u32(flags + i % kSlots * kFlags + (me & 1) * kScouts + q), (me & ~1u) + c), ~kNoFactors, i + 1);
     }
     if ((me & 1) == 0) drain_pair_copies<STAGES>(full, *issued, ld_cluster_s64(mapa_rank(smem_u32(issued), me + 1)), STAGE);
   });
