@@ -39,11 +39,12 @@ template <typename T> struct Per { static constexpr int N = 16 / sizeof(T); };
 // What a lane reads of a run: codes, gradients (raw), the run's scale.
 template <int E> struct Item { uint32_t c[E / 4]; uint4 g; float scale; };
 
-// The largest magnitude of a code whose product with the scale (>= 0) is at most 1 in fp32: [|x^| <= 1] is one comparison of
-// the code's own value.  A power of two: its inverse.
+// The largest magnitude of a code whose product with the scale's is at most 1 in fp32: [|x^| <= 1] is one comparison of the code's own
+// value.  A power of two: its inverse.
 __device__ __forceinline__ float clip_limit(float scale) {
   const uint32_t bits = __float_as_uint(scale);
-  if ((bits & 0x007FFFFFu) == 0 && bits - 0x00800000u < 0x7E000000u) return __uint_as_float((254u << 23) - bits);
+  if ((bits & 0x807FFFFFu) == 0 && bits - 0x00800000u < 0x7E000000u) return __uint_as_float((254u << 23) - bits);
+  scale = fabsf(scale);
   const uint32_t code = to_e4m3x2(1.0f / scale, 0.0f) & 0x7Fu;        // nearest; the one below where that is too large
   const float v = from_e4m3x2(code).x;
   return v * scale > 1.0f && code != 0 ? from_e4m3x2(code - 1).x : v;
@@ -116,8 +117,7 @@ fp8_binarize_backward_rows(const BackArgs a) {
         back[i] = __uint_as_float(gw[i] ^ sign[i]);
       }
     }
-    const float scale = fabsf(l.scale);                              // here and not in fetch, which waits for nothing
-    const float limit = clip_limit(scale);
+    const float limit = clip_limit(l.scale);
     const bool inside = k0 + RUN <= a.K;                             // warp-uniform: every group of the run is whole or ends with it
     float o[E];
 #pragma unroll
@@ -136,7 +136,7 @@ fp8_binarize_backward_rows(const BackArgs a) {
         sb += __shfl_xor_sync(0xffffffffu, sb, off);
       }
       float dm, db;
-      sm *= scale;                                                   // one scale: a group lies in one run of 128
+      sm *= fabsf(l.scale);                                          // one scale: a group lies in one run of 128
       if (inside) {
         dm = sm * (1.0f / BETA); db = sb * (1.0f / BETA);
       } else {
