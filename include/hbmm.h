@@ -460,7 +460,8 @@ hbmm_status hbmm_fp8_input_grad(const hbmm_fp8_operand *GY, const hbmm_fp8_opera
  * GW[n,k] = base[n,k] + sum_m gy[m,n] X^[m,k], X^ = codes times scales: the gradient with respect to the weights from the
  * 8-bit copy of the activations, which is all that the forward pass has to keep of them.
  * gy: device bf16 [M, ldg], ldg >= N, rows on 16-byte boundaries.  X: M x K, block_rows 1.  X^ enters as bf16: exact for
- * scales that are powers of two (what hbmm_fp8_quantize writes), otherwise rounded to nearest even.  Sums in fp32.
+ * the scales that hbmm_fp8_quantize writes (powers of two), otherwise rounded to nearest even.  Sums: the tensor cores' truncating
+ * ones over runs of 512 rows, added in fp32 to nearest.
  * base: fp32 [N, ld_base] or NULL (zeros); it may be GW itself (same address and leading dimension: the gradient is added
  * to what is there) and may not overlap it otherwise.  GW: device fp32 [N, ldw], ldw >= K; base and GW rows on 16-byte
  * boundaries.  Errors: INVALID_ARG, UNSUPPORTED (gy_dtype, block_rows, sizes), ALIGNMENT, CUDA.

@@ -5,13 +5,14 @@
 // A pair of CTAs takes a 256 x 256 tile (cta_group::2, 256 x N x 32 MMAs); how it sums the groups goes by their scales, four groups
 // (a step) at a time:
 //   * all of them powers of two (what hbmm_fp8_quantize writes): the tensor cores apply them (kind::mxf8f6f4, block scales: a UE8M0
-//     byte per row and 32 elements, here the same byte for the four instructions of a group) and the whole walk along K is one
-//     accumulation in tensor memory, 256 columns;
+//     byte per row and 32 elements, here the same byte for the four instructions of a group) and a run along K (kChunk below) is
+//     one accumulation in tensor memory, 256 columns;
 //   * otherwise each group's dot products go to one of three units of 128 columns, and the epilogue adds them, times the two scales,
 //     to fp32 registers.  The accumulation in tensor memory is left where it stands and taken first.
-// The second way costs 560 clk per 128 columns and group, MMA to epilogue and back (8192^3 with scales of any value 0.57 ms, 1.94
-// PFLOP/s; in seven units of 64 columns 1.17 ms); the first is bound by the tensor cores and their power (0.37 to 0.45 ms, 2.98 to 2.45
-// PFLOP/s, by how warm the part is; the MMAs alone 0.29 ms; tensor pipe 82 % active on 2048 x 8192 x 8192).
+// The second way costs 560 clk per 128 columns and group, MMA to epilogue and back (8192^3 with scales of any value 0.57 ms in short
+// runs, 1.94 PFLOP/s, 0.69 in long ones; in seven units of 64 columns 1.17 ms).  The first is bound by the tensor cores' power: 8192^3
+// to bf16 0.38 to 0.39 ms in a run of a few milliseconds, 0.46 (2.4 PFLOP/s) in one of seconds, where the 1000 W hold the SMs at 1160
+// of 1965 MHz; with operands of zeros, which take less, 0.29.  To fp32 0.41 to 0.51.  Tensor pipe 82 % active on 2048 x 8192 x 8192.
 //
 // C = A^ W^ (the input gradient; the contraction runs along the rows of W) reads the same W: its tiles arrive as 128 rows of the
 // contraction x 128 columns and enter the MMA as an MN-major operand.  Nothing is transposed in memory.

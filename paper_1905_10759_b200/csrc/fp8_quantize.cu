@@ -8,7 +8,7 @@
 // group (fp32: the whole warp) or two (bf16: half a warp each), whose maximum is a tree over the raw bits (magnitudes order as their
 // bits do).  The next four loads are in flight meanwhile.
 // Blocks: one CTA per block keeps its raw elements in registers between the maximum and the conversion.
-// Measured: rows, 8192 x 8192 bf16 (203 MB) 39 us, 5.3 TB/s; blocks, 4096 x 9216 fp32 (189 MB) 32 us, 5.8 TB/s.  Two CTAs of the row
+// Measured: rows, 8192 x 8192 bf16 (203 MB) 38 us, 5.3 TB/s, fp32 (338 MB) 57, 5.9; blocks, 4096 x 9216 fp32 (189 MB) 32, 5.8 TB/s.  Two CTAs of the row
 // kernel more per SM with fewer loads each: 41 us and up.
 #include <cuda_bf16.h>
 #include "fp8_common.cuh"

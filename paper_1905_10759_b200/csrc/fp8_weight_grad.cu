@@ -16,9 +16,10 @@
 // The first CTA's MMAs read what the second one's converters wrote.  These arrive at a barrier of their own CTA; a thread that waits
 // there announces the stage by an asynchronous store, whose completion is a release at cluster scope and holds nobody up.  (8192 x
 // 4096 x 4096: 250 us; with that store from the converters 280, with releasing arrivals 443, from the waiting thread 361 to 465.)
-// Measured: 8192 x 4096 x 4096 247 us, 1.11 PFLOP/s (tensor pipe half of the time active: the converters take 930 clk per stage, and
-// copies, conversion and MMA want 160 bytes of shared memory per clock at full rate, of 128); 256 x 4096 x 9216 45 us, 151 MB
-// written; 72 us with a base, 302 MB.
+// Measured: 8192 x 4096 x 4096 250 us in a run of a few milliseconds, 1.1 PFLOP/s, 290 in one of seconds, where the 1000 W hold the SMs
+// at 1630 of 1965 MHz (zeros: 239 at 1965, the same clocks).  Tensor pipe half of the time active: the converters take 930 clk per
+// stage, and copies, conversion and MMA want 160 bytes of shared memory per clock at full rate, of 128.  256 x 4096 x 9216 46 us, 151
+// MB written; 72 us with a base, 302 MB.
 // Few tiles: a cluster of two to four pairs shares each tile in equal parts of m (fp8_tile.cuh).
 #include <cuda_bf16.h>
 #include "fp8_tile.cuh"
