@@ -134,6 +134,7 @@ fp8_gemm_kernel(const Args g, const __grid_constant__ CUtensorMap a_map, const _
     *abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
+  if (tid < kSlots * kFlags) flags[tid] = 0;            // no step's number
   if (warp == kMmaWarp) {
     tmem_alloc_pair(tmem_base_ptr, 512);
     tmem_relinquish_pair();

@@ -325,7 +325,7 @@ __device__ __forceinline__ void drain_pair_copies(uint64_t* full, int64_t issued
     mbar_wait_quiet(bar, static_cast<uint32_t>((i / STAGES) & 1), kDrainPolls);
   }
 }
-// A word that st_async_u32 is bringing to this address of the cluster.
+// A word that st_async_u32 is bringing to this address of the cluster (where the kernel wrote another one at its start).
 __device__ __forceinline__ void wait_word(uint32_t cluster_addr, uint32_t mask, uint32_t value) {
   for (uint32_t it = 0; it < kDrainPolls; it++)
     if ((ld_cluster_u32(cluster_addr) & mask) == value) return;
@@ -344,7 +344,7 @@ static __global__ void wait_expiry_kernel() {
   if (blockIdx.x == 0) wait(smem_u32(&bar), 0, 9);
   else wait.cluster(smem_u32(&bar), 0, 9);
 }
-inline cudaError_t launch_wait_expiry(cudaStream_t stream) {
+static inline cudaError_t launch_wait_expiry(cudaStream_t stream) {
   wait_expiry_kernel<<<2, 32, 0, stream>>>();
   return cudaGetLastError();
 }

@@ -98,6 +98,7 @@ fp8_weight_grad_kernel(const Args g, const __grid_constant__ CUtensorMap gy_map,
     *abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
+  if (tid < STAGES) told[tid] = 0;
   if (warp == kMmaWarp) {
     tmem_alloc_pair(tmem_base_ptr, 512);
     tmem_relinquish_pair();
